@@ -61,8 +61,10 @@ typedef enum {
   TDN_ERR_BAD_GEOMETRY = 10,       /* radius graph: graph_ptr, positions or box   */
   TDN_ERR_EDGE_CAPACITY = 11,      /* radius graph: more edges than buffer room   */
   TDN_ERR_NEIGHBOUR_LIMIT = 12,    /* radius graph: > 2048 candidates for an atom */
-  TDN_ERR_SCRATCH_LIMIT = 13       /* no-allocation forward: workspace needed
+  TDN_ERR_SCRATCH_LIMIT = 13,      /* no-allocation forward: workspace needed
                                       above TDN_NOALLOC_SCRATCH_BYTES           */
+  TDN_ERR_MISALIGNED = 14          /* layer norm, feed-forward block, attention
+                                      backward: a pointer not 16-byte aligned   */
 } tdn_status;
 
 typedef enum { TDN_F32 = 0, TDN_BF16 = 1 } tdn_dtype;
@@ -381,6 +383,84 @@ tdn_status tdn_ps_linear_workspace_size(int32_t C, int32_t w_dtype, size_t* byte
 tdn_status tdn_ps_linear(int32_t n_nodes, int32_t L, int32_t C, const float* x, const void* W, int32_t w_dtype,
                          float* y, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* Equivariant layer norm (the norm of the transformer block around the layer,
+ * Sec. 4.1 "Model Design"; the paper gives no equations, this is the reading
+ * implemented).  Per node and degree l, over the degree's 2l + 1 rows and C
+ * channels of x [N, d, C], with xc = x less its mean over channels for l = 0
+ * and xc = x for l > 0 (a mean over components would not commute with
+ * rotations):
+ *   y^(l) = gamma[l] * xc / sqrt(mean(xc^2) + eps)   (+ beta for l = 0)
+ * L = 0 is the layer norm of C-vectors.
+ *   x, y   [N, d, C]    dtype (TDN_F32 or TDN_BF16; statistics are f32, y is
+ *                       rounded once)
+ *   gamma  [L + 1, C]   f32
+ *   beta   [C]          f32 or NULL (no shift)
+ * 0 <= L <= 6, C in 16..256 with C % 16 = 0, eps > 0 (TDN_ERR_BAD_SHAPE).
+ * n_nodes = 0 is a no-op.  y may be x. */
+tdn_status tdn_layer_norm_forward(int32_t n_nodes, int32_t L, int32_t C, int32_t dtype, float eps, const void* x,
+                                  const float* gamma, const float* beta, void* y, hipStream_t stream);
+
+/* Its backward for the scalar <grad_y, y>; the statistics are recomputed from
+ * x.  grad_y, grad_res and grad_x have dtype; grad_res, if not NULL, is added
+ * to grad_x (the gradient of the skip connection around the norm).  Any output
+ * may be NULL:
+ *   grad_x     [N, d, C]   dtype
+ *   grad_gamma [L + 1, C]  f32, summed over nodes in a fixed order
+ *   grad_beta  [C]         f32, likewise
+ * Outputs must not overlap inputs.  Workspace from
+ * tdn_layer_norm_workspace_size. */
+tdn_status tdn_layer_norm_workspace_size(int32_t n_nodes, int32_t L, int32_t C, size_t* bytes);
+tdn_status tdn_layer_norm_backward(int32_t n_nodes, int32_t L, int32_t C, int32_t dtype, float eps, const void* x,
+                                   const float* gamma, const void* grad_y, const void* grad_res, void* grad_x,
+                                   float* grad_gamma, float* grad_beta, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
+/* Gated feed-forward block (the feed-forward block that follows the attention
+ * block, Sec. 4.1 "Model Design", with one matrix for every degree as in
+ * tdn_ps_linear, Sec. 3.2; the paper gives no equations, this is the reading
+ * implemented):
+ *   u = x w_up                       [N, d, F]
+ *   q = x^(0) w_gate + b_gate        [N, F], from the invariant rows alone
+ *   y = (u * act(q)) w_down (+ residual)
+ * with a node's gate shared by its d rows, so that y rotates with x.  L = 0 is
+ * the gated feed-forward block of C-vectors.  Every tensor but b_gate has the
+ * problem's dtype.
+ *   x, residual, y [N, d, C]   residual may be NULL; y may be residual
+ *   w_up, w_gate   [C, F]
+ *   w_down         [F, C]
+ *   b_gate         [F] f32 or NULL
+ * TDN_F32: fp32-level accuracy (16-bit MFMA over two-part splits).  TDN_BF16:
+ * bf16 MFMA with fp32 accumulation; u * act(q) is rounded to bf16 once, y once.
+ * C in 16..256 and F in 16..4096, multiples of 16, 0 <= L <= 6
+ * (TDN_ERR_BAD_SHAPE, also for an unknown activation).  n_nodes = 0 is a
+ * no-op.  Workspace from tdn_gated_ffn_workspace_size (either pointer may be
+ * NULL). */
+typedef enum { TDN_ACT_SILU = 0, TDN_ACT_GELU = 1, TDN_ACT_SIGMOID = 2 } tdn_activation; /* GELU: with erf */
+typedef struct {
+  int32_t n_nodes;  /* N >= 0                        */
+  int32_t L;        /* d = (L + 1)^2 rows a node      */
+  int32_t C;        /* channels                       */
+  int32_t n_hidden; /* F                              */
+  int32_t dtype;    /* tdn_dtype                      */
+  int32_t act;      /* tdn_activation of the gate     */
+} tdn_ffn_problem;
+tdn_status tdn_gated_ffn_workspace_size(const tdn_ffn_problem* p, size_t* fwd_bytes, size_t* bwd_bytes);
+tdn_status tdn_gated_ffn_forward(const tdn_ffn_problem* p, const void* x, const void* w_up, const void* w_gate,
+                                 const float* b_gate, const void* w_down, const void* residual, void* y,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Its backward for the scalar <grad_y, y>: u, q and the hidden values are
+ * recomputed (the forward saves nothing; residual's gradient is grad_y).  Any
+ * output may be NULL: grad_x [N, d, C], grad_w_up and grad_w_gate [C, F] and
+ * grad_w_down [F, C] in the problem's dtype, grad_b_gate [F] f32.  With
+ * TDN_BF16, u * act(q), (grad_y w_down^T) * act(q) and dq are each rounded to
+ * bf16 once, the outputs once.  Sums over nodes run in a fixed order.  Outputs
+ * must not overlap inputs.  n_nodes = 0 zeroes the weights' gradients. */
+tdn_status tdn_gated_ffn_backward(const tdn_ffn_problem* p, const void* x, const void* w_up, const void* w_gate,
+                                  const float* b_gate, const void* w_down, const void* grad_y, void* grad_x,
+                                  void* grad_w_up, void* grad_w_gate, float* grad_b_gate, void* grad_w_down,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Real spherical harmonics of edge directions (basis as above; the
  * harmonics input of the tensor product, Sec. 2, which the CP layer
  * contracts with its factor B, Sec. 3.1 eq. approximate), and their
@@ -400,6 +480,7 @@ tdn_status tdn_spherical_harmonics(int32_t L, int32_t E, const float* edge_vec, 
  * "dense_edge_fwd", "dense_edge_unshared",
  * "path_gemm", "radius_graph", "edge_factors" (the launch before the layout where an edge pass
  * goes through per-edge matrices), "feature_layout",
+ * "layer_norm", "layer_norm_bwd", "gated_ffn", "gated_ffn_bwd",
  * "channel_layout", "cp_edge_bwd_src", "cp_bwd_dst", "radial_grad", "node_gemm", "gram",
  * "sort");
  * reset = 1 clears that kernel's record. */

@@ -12,14 +12,17 @@ the library is not built -- there is no fallback implementation.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 
 import torch
 
 __all__ = ["forward", "backward", "sort_by_key", "spherical_harmonics", "workspace_size", "Problem",
-           "TdnError", "lib", "timer_enable", "timer_read", "LIB_PATH", "status_string"]
+           "TdnError", "layer_norm", "layer_norm_backward", "gated_ffn", "gated_ffn_backward", "lib", "timer_enable",
+           "timer_read", "LIB_PATH", "status_string"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtdn.so")
 
@@ -28,7 +31,7 @@ STATUS = {0: "TDN_OK", 1: "TDN_ERR_NULL_POINTER", 2: "TDN_ERR_BAD_SHAPE", 3: "TD
           4: "TDN_ERR_WORKSPACE_TOO_SMALL", 5: "TDN_ERR_INDEX_OUT_OF_RANGE", 6: "TDN_ERR_NOT_SORTED",
           7: "TDN_ERR_DEGENERATE_EDGE", 8: "TDN_ERR_UNSUPPORTED_DEVICE", 9: "TDN_ERR_HIP",
           10: "TDN_ERR_BAD_GEOMETRY", 11: "TDN_ERR_EDGE_CAPACITY", 12: "TDN_ERR_NEIGHBOUR_LIMIT",
-          13: "TDN_ERR_SCRATCH_LIMIT"}
+          13: "TDN_ERR_SCRATCH_LIMIT", 14: "TDN_ERR_MISALIGNED"}
 TDN_ERR_EDGE_CAPACITY = 11
 
 
@@ -39,6 +42,11 @@ class TdnError(RuntimeError):
         if status == 9:
             extra = f" (hipError {lib().tdn_last_hip_error()})"
         super().__init__(f"{where}: {STATUS.get(status, status)}{extra}")
+
+
+class FfnProblem(ctypes.Structure):
+    _fields_ = [("n_nodes", ctypes.c_int32), ("L", ctypes.c_int32), ("C", ctypes.c_int32),
+                ("n_hidden", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
 
 
 class GraphProblem(ctypes.Structure):
@@ -85,6 +93,13 @@ def lib() -> ctypes.CDLL:
         L.tdn_radius_graph_workspace_size.argtypes = [GP, ctypes.POINTER(_SZ)]
         L.tdn_radius_graph.argtypes = [GP, _P, _P, _P, ctypes.c_int64, _P, _P, _P, _P,
                                        ctypes.POINTER(ctypes.c_int64), _P, _SZ, _P]
+        I32, F32, FP = ctypes.c_int32, ctypes.c_float, ctypes.POINTER(FfnProblem)
+        L.tdn_layer_norm_forward.argtypes = [I32] * 4 + [F32] + [_P] * 5
+        L.tdn_layer_norm_workspace_size.argtypes = [I32] * 3 + [ctypes.POINTER(_SZ)]
+        L.tdn_layer_norm_backward.argtypes = [I32] * 4 + [F32] + [_P] * 8 + [_SZ, _P]
+        L.tdn_gated_ffn_workspace_size.argtypes = [FP, ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)]
+        L.tdn_gated_ffn_forward.argtypes = [FP] + [_P] * 8 + [_SZ, _P]
+        L.tdn_gated_ffn_backward.argtypes = [FP] + [_P] * 12 + [_SZ, _P]
         L.tdn_sort_workspace_size.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(_SZ)]
         L.tdn_sort_by_key.argtypes = [ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _SZ, _P]
         L.tdn_spherical_harmonics.argtypes = [ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P]
@@ -101,7 +116,9 @@ def lib() -> ctypes.CDLL:
                   "tdn_cp_tp3_forward", "tdn_ps_linear_workspace_size", "tdn_ps_linear",
                   "tdn_dense_tp_unshared_workspace_size", "tdn_dense_tp_forward_unshared",
                   "tdn_ablation_workspace_size", "tdn_ablation_forward", "tdn_attention_workspace_size",
-                  "tdn_attention_forward"):
+                  "tdn_attention_forward", "tdn_layer_norm_forward", "tdn_layer_norm_workspace_size",
+                  "tdn_layer_norm_backward", "tdn_gated_ffn_workspace_size", "tdn_gated_ffn_forward",
+                  "tdn_gated_ffn_backward"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -331,6 +348,168 @@ def ps_linear(x, W, *, workspace=None, out=None, stream=None):
     _check(lib().tdn_ps_linear(N, L, C, _ptr(x), _ptr(W), wd, _ptr(out), _ptr(workspace), workspace.numel(),
                                _stream(stream)), "tdn_ps_linear")
     return out
+
+
+@contextlib.contextmanager
+def _launching(dev, stream):
+    """The tensors' device and the stream made current (the given stream, or
+    the device's current one), so that scratch memory allocated inside belongs
+    to the stream that uses it."""
+    if dev.type != "cuda":
+        raise ValueError(f"tensors on {dev}: the library runs on a GPU")
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device != dev:
+        raise ValueError(f"stream on {stream.device}, tensors on {dev}")
+    with torch.cuda.stream(stream):     # (sets the device too)
+        yield stream
+
+
+def _feature_dtype(x, name="x"):
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    if x.dim() != 3:
+        raise ValueError(f"{name} must be [N, (L+1)^2, C]")
+    L = math.isqrt(x.shape[1]) - 1
+    if L < 0 or (L + 1) ** 2 != x.shape[1]:
+        raise ValueError(f"{name} must be [N, (L+1)^2, C]")
+    return L, TDN_BF16 if x.dtype == torch.bfloat16 else TDN_F32
+
+
+def _workspace(workspace, nbytes, dev):
+    if workspace is None or workspace.numel() * workspace.element_size() < nbytes:
+        return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {dev}")
+    return workspace
+
+
+def layer_norm(x, gamma, beta=None, *, eps: float = 1e-5, out=None, stream=None):
+    """Runs tdn_layer_norm_forward, the equivariant layer norm: per node and
+    degree l, x^(l) (less its channel mean for l = 0) over the root of its mean
+    square, times gamma[l] (plus beta for l = 0).  x [N, (L+1)^2, C] float32 or
+    bfloat16, gamma [L+1, C] and beta [C] float32; returns y like x."""
+    L, dt = _feature_dtype(x)
+    N, d, C = x.shape
+    dev = x.device
+    _need(x, "x", x.dtype, (N, d, C), dev)
+    _need(gamma, "gamma", torch.float32, (L + 1, C), dev)
+    if beta is not None:
+        _need(beta, "beta", torch.float32, (C,), dev)
+    if out is not None:
+        _need(out, "out", x.dtype, (N, d, C), dev)
+    with _launching(dev, stream) as s:
+        if out is None:
+            out = torch.empty_like(x)
+        _check(lib().tdn_layer_norm_forward(N, L, C, dt, float(eps), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(out),
+                                            _stream(s)), "tdn_layer_norm_forward")
+    return out
+
+
+def layer_norm_backward(x, gamma, grad_y, *, eps: float = 1e-5, grad_res=None, need_x=True, need_weights=True,
+                        workspace=None, stream=None):
+    """Runs tdn_layer_norm_backward: (grad_x like x, grad_gamma [L+1, C],
+    grad_beta [C]), None where not needed.  grad_y like x; grad_res, like x, is
+    added to grad_x (the gradient that reaches x past the norm)."""
+    L, dt = _feature_dtype(x)
+    N, d, C = x.shape
+    dev = x.device
+    _need(x, "x", x.dtype, (N, d, C), dev)
+    _need(gamma, "gamma", torch.float32, (L + 1, C), dev)
+    _need(grad_y, "grad_y", x.dtype, (N, d, C), dev)
+    if grad_res is not None:
+        _need(grad_res, "grad_res", x.dtype, (N, d, C), dev)
+    with _launching(dev, stream) as s:
+        nb = _SZ()
+        _check(lib().tdn_layer_norm_workspace_size(N, L, C, ctypes.byref(nb)), "tdn_layer_norm_workspace_size")
+        workspace = _workspace(workspace, nb.value, dev)
+        gx = torch.empty_like(x) if need_x else None
+        gg = torch.empty((L + 1, C), dtype=torch.float32, device=dev) if need_weights else None
+        gb = torch.empty((C,), dtype=torch.float32, device=dev) if need_weights else None
+        _check(lib().tdn_layer_norm_backward(N, L, C, dt, float(eps), _ptr(x), _ptr(gamma), _ptr(grad_y),
+                                             _ptr(grad_res), _ptr(gx), _ptr(gg), _ptr(gb), _ptr(workspace),
+                                             workspace.numel() * workspace.element_size(), _stream(s)),
+               "tdn_layer_norm_backward")
+    return gx, gg, gb
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "sigmoid": 2}
+
+
+def make_ffn_problem(n_nodes, L, C, n_hidden, dtype=TDN_F32, activation="silu") -> FfnProblem:
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    return FfnProblem(int(n_nodes), int(L), int(C), int(n_hidden), int(dtype), ACTIVATIONS[activation])
+
+
+def gated_ffn_workspace_size(p: FfnProblem) -> tuple[int, int]:
+    """Workspace bytes of tdn_gated_ffn_forward and tdn_gated_ffn_backward."""
+    f, b = _SZ(), _SZ()
+    _check(lib().tdn_gated_ffn_workspace_size(ctypes.byref(p), ctypes.byref(f), ctypes.byref(b)),
+           "tdn_gated_ffn_workspace_size")
+    return f.value, b.value
+
+
+def _ffn_arguments(x, w_up, w_gate, w_down, b_gate, activation):
+    L, dt = _feature_dtype(x)
+    N, d, C = x.shape
+    if not isinstance(w_up, torch.Tensor) or w_up.dim() != 2:
+        raise ValueError("w_up must be [C, F]")
+    F = w_up.shape[1]
+    for t, n, sh in [(x, "x", (N, d, C)), (w_up, "w_up", (C, F)), (w_gate, "w_gate", (C, F)),
+                     (w_down, "w_down", (F, C))]:
+        _need(t, n, x.dtype, sh, x.device)
+    if b_gate is not None:
+        _need(b_gate, "b_gate", torch.float32, (F,), x.device)
+    return make_ffn_problem(N, L, C, F, dt, activation)
+
+
+def gated_ffn(x, w_up, w_gate, w_down, *, b_gate=None, residual=None, activation="silu", workspace=None, out=None,
+              stream=None):
+    """Runs tdn_gated_ffn_forward, y = ((x w_up) * act(x[:, 0] w_gate + b_gate)) w_down + residual:
+    the gate comes from the invariant row and is shared by a node's d rows.  x
+    [N, (L+1)^2, C], w_up and w_gate [C, F], w_down [F, C] and residual like x,
+    all float32 or all bfloat16; b_gate [F] float32; activation "silu", "gelu"
+    or "sigmoid".  Returns y like x (out may be residual)."""
+    p = _ffn_arguments(x, w_up, w_gate, w_down, b_gate, activation)
+    dev = x.device
+    for t, n in [(residual, "residual"), (out, "out")]:
+        if t is not None:
+            _need(t, n, x.dtype, tuple(x.shape), dev)
+    if out is not None and out.numel() and out.data_ptr() == x.data_ptr():
+        raise ValueError("out must not be x")
+    with _launching(dev, stream) as s:
+        workspace = _workspace(workspace, gated_ffn_workspace_size(p)[0], dev)
+        if out is None:
+            out = torch.empty_like(x)
+        _check(lib().tdn_gated_ffn_forward(ctypes.byref(p), _ptr(x), _ptr(w_up), _ptr(w_gate), _ptr(b_gate),
+                                           _ptr(w_down), _ptr(residual), _ptr(out), _ptr(workspace),
+                                           workspace.numel() * workspace.element_size(), _stream(s)),
+               "tdn_gated_ffn_forward")
+    return out
+
+
+def gated_ffn_backward(x, w_up, w_gate, w_down, grad_y, *, b_gate=None, activation="silu", need_x=True,
+                       need_weights=True, workspace=None, stream=None):
+    """Runs tdn_gated_ffn_backward: (grad_x, grad_w_up, grad_w_gate,
+    grad_w_down, grad_b_gate), each like its input, None where not needed
+    (grad_b_gate also without b_gate).  The residual's gradient is grad_y."""
+    p = _ffn_arguments(x, w_up, w_gate, w_down, b_gate, activation)
+    dev = x.device
+    _need(grad_y, "grad_y", x.dtype, tuple(x.shape), dev)
+    with _launching(dev, stream) as s:
+        workspace = _workspace(workspace, gated_ffn_workspace_size(p)[1], dev)
+        gx = torch.empty_like(x) if need_x else None
+        gu, gg, gd = (torch.empty_like(w) if need_weights else None for w in (w_up, w_gate, w_down))
+        gb = torch.empty_like(b_gate) if need_weights and b_gate is not None else None
+        _check(lib().tdn_gated_ffn_backward(ctypes.byref(p), _ptr(x), _ptr(w_up), _ptr(w_gate), _ptr(b_gate),
+                                            _ptr(w_down), _ptr(grad_y), _ptr(gx), _ptr(gu), _ptr(gg), _ptr(gb),
+                                            _ptr(gd), _ptr(workspace),
+                                            workspace.numel() * workspace.element_size(), _stream(s)),
+               "tdn_gated_ffn_backward")
+    return gx, gu, gg, gd, gb
 
 
 @dataclass

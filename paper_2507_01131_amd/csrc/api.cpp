@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -400,6 +401,7 @@ const char* tdn_status_string(tdn_status s) {
     case TDN_ERR_BAD_GEOMETRY: return "invalid graph_ptr, position or periodic box";
     case TDN_ERR_EDGE_CAPACITY: return "edge buffers smaller than the edge count";
     case TDN_ERR_NEIGHBOUR_LIMIT: return "more than 2048 neighbours of one atom within the cutoff";
+    case TDN_ERR_MISALIGNED: return "pointer not 16-byte aligned";
     case TDN_ERR_SCRATCH_LIMIT:
       return "the problem needs more workspace than the no-allocation entry point's fixed scratch area holds";
   }
@@ -715,6 +717,149 @@ tdn_status tdn_ps_linear(int32_t n_nodes, int32_t L, int32_t C, const float* x, 
   if (n_nodes == 0) return TDN_OK;
   Timed t("node_gemm", stream);
   TDN_HIP(tdn::launch_node_gemm(n_nodes * dim_of(L), C, x, W, !f32, 0, y, workspace, stream));
+  return TDN_OK;
+}
+
+namespace {
+// whether every pointer is 16-byte aligned (NULL is)
+bool aligned16(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return false;
+  return true;
+}
+tdn_status check_norm(int32_t n_nodes, int32_t L, int32_t C) {
+  if (n_nodes < 0 || L < 0 || L > 6 || C < 16 || C > 256 || C % 16 != 0) return TDN_ERR_BAD_SHAPE;
+  if (int64_t(n_nodes) * dim_of(L) >= (int64_t(1) << 31) - 4096) return TDN_ERR_BAD_SHAPE;
+  return TDN_OK;
+}
+tdn_status check_norm_call(int32_t n_nodes, int32_t L, int32_t C, int32_t dtype, float eps) {
+  if (dtype != TDN_F32 && dtype != TDN_BF16) return TDN_ERR_BAD_DTYPE;
+  if (!(eps > 0.f) || !std::isfinite(eps)) return TDN_ERR_BAD_SHAPE;
+  return check_norm(n_nodes, L, C);
+}
+}  // namespace
+
+tdn_status tdn_layer_norm_forward(int32_t n_nodes, int32_t L, int32_t C, int32_t dtype, float eps, const void* x,
+                                  const float* gamma, const float* beta, void* y, hipStream_t stream) {
+  tdn_status st = check_norm_call(n_nodes, L, C, dtype, eps);
+  if (st != TDN_OK) return st;
+  if (!gamma || (n_nodes > 0 && (!x || !y))) return TDN_ERR_NULL_POINTER;
+  if (!aligned16({x, gamma, beta, y})) return TDN_ERR_MISALIGNED;
+  st = check_device();
+  if (st != TDN_OK) return st;
+  Timed t("layer_norm", stream);
+  TDN_HIP(tdn::launch_layer_norm(n_nodes, L, C, dtype == TDN_BF16, eps, x, gamma, beta, y, stream));
+  return TDN_OK;
+}
+
+tdn_status tdn_layer_norm_workspace_size(int32_t n_nodes, int32_t L, int32_t C, size_t* bytes) {
+  const tdn_status st = check_norm(n_nodes, L, C);
+  if (st != TDN_OK) return st;
+  if (!bytes) return TDN_ERR_NULL_POINTER;
+  *bytes = al(size_t(tdn::layer_norm_parts(n_nodes, C)) * (L + 2) * C * 4);
+  return TDN_OK;
+}
+
+tdn_status tdn_layer_norm_backward(int32_t n_nodes, int32_t L, int32_t C, int32_t dtype, float eps, const void* x,
+                                   const float* gamma, const void* grad_y, const void* grad_res, void* grad_x,
+                                   float* grad_gamma, float* grad_beta, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream) {
+  tdn_status st = check_norm_call(n_nodes, L, C, dtype, eps);
+  if (st != TDN_OK) return st;
+  const bool sums = n_nodes > 0 && (grad_gamma || grad_beta);
+  if (!gamma || (n_nodes > 0 && (!x || !grad_y)) || (sums && !workspace)) return TDN_ERR_NULL_POINTER;
+  if (!aligned16({x, gamma, grad_y, grad_res, grad_x, grad_gamma, grad_beta, workspace}))
+    return TDN_ERR_MISALIGNED;
+  if (sums && workspace_bytes < size_t(tdn::layer_norm_parts(n_nodes, C)) * (L + 2) * C * 4)
+    return TDN_ERR_WORKSPACE_TOO_SMALL;
+  st = check_device();
+  if (st != TDN_OK) return st;
+  Timed t("layer_norm_bwd", stream);
+  TDN_HIP(tdn::launch_layer_norm_bwd(n_nodes, L, C, dtype == TDN_BF16, eps, x, gamma, grad_y, grad_res, grad_x,
+                                     grad_gamma, grad_beta, static_cast<float*>(workspace), stream));
+  return TDN_OK;
+}
+
+namespace {
+tdn_status check_ffn(const tdn_ffn_problem* p) {
+  if (!p) return TDN_ERR_NULL_POINTER;
+  if (p->dtype != TDN_F32 && p->dtype != TDN_BF16) return TDN_ERR_BAD_DTYPE;
+  const tdn_status st = check_norm(p->n_nodes, p->L, p->C);
+  if (st != TDN_OK) return st;
+  if (p->n_hidden < 16 || p->n_hidden > 4096 || p->n_hidden % 16 != 0) return TDN_ERR_BAD_SHAPE;
+  if (p->act != TDN_ACT_SILU && p->act != TDN_ACT_GELU && p->act != TDN_ACT_SIGMOID) return TDN_ERR_BAD_SHAPE;
+  return TDN_OK;
+}
+tdn::FfnShape ffn_shape(const tdn_ffn_problem& p) {
+  static_assert(TDN_ACT_SILU == tdn::kActSilu && TDN_ACT_GELU == tdn::kActGelu && TDN_ACT_SIGMOID == tdn::kActSigmoid,
+                "the kernels' activation codes");
+  return {p.n_nodes, dim_of(p.L), p.C, p.n_hidden, p.act, p.dtype == TDN_BF16};
+}
+}  // namespace
+
+tdn_status tdn_gated_ffn_workspace_size(const tdn_ffn_problem* p, size_t* fwd_bytes, size_t* bwd_bytes) {
+  const tdn_status st = check_ffn(p);
+  if (st != TDN_OK) return st;
+  if (fwd_bytes) *fwd_bytes = tdn::gated_ffn_ws_bytes(ffn_shape(*p), false);
+  if (bwd_bytes) *bwd_bytes = tdn::gated_ffn_ws_bytes(ffn_shape(*p), true);
+  return TDN_OK;
+}
+
+tdn_status tdn_gated_ffn_forward(const tdn_ffn_problem* p, const void* x, const void* w_up, const void* w_gate,
+                                 const float* b_gate, const void* w_down, const void* residual, void* y,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  tdn_status st = check_ffn(p);
+  if (st != TDN_OK) return st;
+  if (!w_up || !w_gate || !w_down || !workspace || (p->n_nodes > 0 && (!x || !y))) return TDN_ERR_NULL_POINTER;
+  if (!aligned16({x, w_up, w_gate, b_gate, w_down, residual, y, workspace}))
+    return TDN_ERR_MISALIGNED;
+  const tdn::FfnShape sh = ffn_shape(*p);
+  if (workspace_bytes < tdn::gated_ffn_ws_bytes(sh, false)) return TDN_ERR_WORKSPACE_TOO_SMALL;
+  st = check_device();
+  if (st != TDN_OK) return st;
+  tdn::FfnArgs a{};
+  a.x = x;
+  a.w_up = w_up;
+  a.w_gate = w_gate;
+  a.w_down = w_down;
+  a.b_gate = b_gate;
+  a.residual = residual;
+  a.y = y;
+  a.ws = workspace;
+  Timed t("gated_ffn", stream);
+  TDN_HIP(tdn::launch_gated_ffn(sh, a, stream));
+  return TDN_OK;
+}
+
+tdn_status tdn_gated_ffn_backward(const tdn_ffn_problem* p, const void* x, const void* w_up, const void* w_gate,
+                                  const float* b_gate, const void* w_down, const void* grad_y, void* grad_x,
+                                  void* grad_w_up, void* grad_w_gate, float* grad_b_gate, void* grad_w_down,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  tdn_status st = check_ffn(p);
+  if (st != TDN_OK) return st;
+  if (!w_up || !w_gate || !w_down || !workspace || (p->n_nodes > 0 && (!x || !grad_y))) return TDN_ERR_NULL_POINTER;
+  if (!aligned16({x, w_up, w_gate, b_gate, w_down, grad_y, grad_x, grad_w_up, grad_w_gate, grad_b_gate, grad_w_down,
+                  workspace}))
+    return TDN_ERR_MISALIGNED;
+  const tdn::FfnShape sh = ffn_shape(*p);
+  if (workspace_bytes < tdn::gated_ffn_ws_bytes(sh, true)) return TDN_ERR_WORKSPACE_TOO_SMALL;
+  st = check_device();
+  if (st != TDN_OK) return st;
+  tdn::FfnArgs a{};
+  a.x = x;
+  a.w_up = w_up;
+  a.w_gate = w_gate;
+  a.w_down = w_down;
+  a.b_gate = b_gate;
+  a.grad_y = grad_y;
+  a.grad_x = grad_x;
+  a.grad_w_up = grad_w_up;
+  a.grad_w_gate = grad_w_gate;
+  a.grad_w_down = grad_w_down;
+  a.grad_b_gate = grad_b_gate;
+  a.ws = workspace;
+  Timed t("gated_ffn_bwd", stream);
+  TDN_HIP(tdn::launch_gated_ffn_bwd(sh, a, stream));
   return TDN_OK;
 }
 

@@ -1,0 +1,1065 @@
+// Gated feed-forward block over node features and its backward.
+//
+//   u = x W_up  [N, d, F],  q = x[:, 0] W_gate + b,  s = act(q)  [N, F],
+//   h = u s (the same s for a node's d rows),  y = h W_down (+ residual).
+// Backward, with dh = grad_y W_down^T:
+//   grad_x = (dh s) W_up^T (+ dq W_gate^T on the degree-0 rows),
+//   dq = act'(q) sum over the node's rows of dh u,
+//   grad W_up = x^T (dh s), grad W_down = h^T grad_y, grad W_gate = x[:, 0]^T dq.
+//
+// Nothing of size [N, d, F] goes to memory.  The forward (k_ffn_rows) takes F
+// in tiles of 32: a wave computes u^T of a tile for its rows (hidden units in
+// the accumulator's registers, rows in lanes), multiplies by s, and the
+// registers regroup into the operand of the second product (the K order
+// acc_krow), which adds into y^T.  grad_x is the same map with the weights'
+// parts exchanged, (grad_y W_down^T, s, W_up^T), so the same kernel runs it.
+// The weights' gradients sum over rows: k_ffn_wgrad keeps [C, 32] sums in
+// registers per tile of F and passes over a range of rows, recomputing u and
+// dh; waves come in pairs, one for u and grad W_down, one for dh and grad
+// W_up, which exchange u through LDS for dq.  The ranges' sums are added in
+// range order.
+//
+// Arithmetic.  fp32 problems: 32x32x16 fp16 MFMA over two-part splits (three
+// part products) of operands scaled by powers of two: rows of x and grad_y by
+// their largest magnitudes, the packed weights per tile of F, and the second
+// product's operand by a running exponent per row (per hidden unit in
+// k_ffn_wgrad) that only grows; the sums are rescaled when it does.  bf16
+// problems: 32x32x16 bf16 MFMA; h, dh s and dq are rounded to bf16 once, as
+// operands; u, dh, q, s and all sums stay fp32.
+#include "common.hpp"
+#include "kernels.h"
+
+namespace tdn {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kBlk = 64;  // u32x4 words of an operand block: 64 lanes x 8 values of 16 bits
+constexpr int kUnset = -1000;  // exponent of a sum that holds nothing yet
+
+template <bool BF>
+__device__ __forceinline__ f32x16 mm(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                  0);
+}
+// the part products of one K-step
+template <bool BF>
+__device__ __forceinline__ f32x16 mm_parts(const u32x4* a, const u32x4* b, f32x16 c) {
+  if constexpr (!BF) {
+    c = mm<BF>(a[1], b[0], c);
+    c = mm<BF>(a[0], b[1], c);
+  }
+  return mm<BF>(a[0], b[0], c);
+}
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+template <bool BF>
+__device__ __forceinline__ f32x4 load4(const void* p, size_t i) {
+  if constexpr (BF) {
+    const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+    return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                 __uint_as_float(u.y & 0xffff0000u)};
+  } else {
+    return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+  }
+}
+template <bool BF>
+__device__ __forceinline__ void store4(void* p, size_t i, f32x4 v) {
+  if constexpr (BF)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =
+        uint2{pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
+  else
+    *reinterpret_cast<f32x4*>(static_cast<float*>(p) + i) = v;
+}
+
+// act(q) and act'(q)
+__device__ __forceinline__ void gate_act(float q, int act, float& s, float& ds) {
+  if (act == kActGelu) {
+    const float cdf = 0.5f * (1.f + erff(q * 0.70710678118654752f));
+    s = q * cdf;
+    ds = fmaf(q * 0.39894228040143268f, expf(-0.5f * q * q), cdf);
+    return;
+  }
+  const float sig = 1.f / (1.f + expf(-q));
+  if (act == kActSigmoid) {
+    s = sig;
+    ds = sig * (1.f - sig);
+  } else {
+    s = q * sig;
+    ds = sig * fmaf(q, 1.f - sig, 1.f);
+  }
+}
+
+// A row's C channels as the operand whose K runs over channels: lane (h, l32)
+// of K-step st holds channels 16 st + 8 h .. + 7 of its row, in parts scaled
+// by 2^-e (fp32 problems; e returned).  row = nullptr: zeros.
+template <int CT, bool BF>
+__device__ __forceinline__ int load_row(const void* base, bool on, size_t at, int C, int h,
+                                        u32x4 (&op)[2 * CT][BF ? 1 : 2]) {
+  if constexpr (BF) {
+#pragma unroll
+    for (int st = 0; st < 2 * CT; ++st)
+      op[st][0] = on && 16 * st < C ? *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at +
+                                                                      16 * st + 8 * h)
+                                    : u32x4{};
+    return 0;
+  } else {
+    f32x4 v[2 * CT][2];
+    float mx = 0.f;
+#pragma unroll
+    for (int st = 0; st < 2 * CT; ++st)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        v[st][k] = on && 16 * st < C
+                       ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at + 16 * st + 8 * h + 4 * k)
+                       : f32x4{};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fabsf(v[st][k][i]));
+      }
+    mx = fmaxf(mx, other_half(mx));
+    const int e = f16_split_exponent(mx);
+    const float sc = ldexpf(1.f, -e);
+#pragma unroll
+    for (int st = 0; st < 2 * CT; ++st)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t hi, lo;
+        split_f16x2_pair(v[st][k >> 1][2 * (k & 1)] * sc, v[st][k >> 1][2 * (k & 1) + 1] * sc, hi, lo);
+        op[st][0][k] = hi;
+        op[st][1][k] = lo;
+      }
+    return e;
+  }
+}
+
+// Sixteen accumulator values of a lane's column as the second product's
+// operand (two K-steps).  fp32 problems: scaled by 2^-(E - bias), E the
+// column's running exponent, with `grow` called on the factor that takes the
+// column's sums to a larger E.
+template <bool BF, typename Grow>
+__device__ __forceinline__ void to_operand(const float (&t)[16], int bias, int& E, u32x4 (&op)[2][BF ? 1 : 2],
+                                           Grow grow) {
+  if constexpr (BF) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) op[q][0][k] = pack_bf16x2_rne(t[8 * q + 2 * k], t[8 * q + 2 * k + 1]);
+  } else {
+    float mx = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, fabsf(t[v]));
+    mx = fmaxf(mx, other_half(mx));
+    const int e = f16_split_exponent(mx) + bias;
+    const bool up = mx > 0.f && e > E;
+    if (__any(up)) {
+      const int to = up ? e : E;
+      grow(ldexpf(1.f, E - to));
+      E = to;
+    }
+    // (a column of zeros may come before its exponent is set)
+    const float sc = ldexpf(1.f, min(bias - E, 126));
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t hi, lo;
+        split_f16x2_pair(t[8 * q + 2 * k] * sc, t[8 * q + 2 * k + 1] * sc, hi, lo);
+        op[q][0][k] = hi;
+        op[q][1][k] = lo;
+      }
+  }
+}
+
+// ------------------------------------------------------------------ weights
+// A weight matrix given as w(c, f) = W[c sc + f sf], packed per tile ft of 32
+// hidden units (zero beyond C and F):
+//   up:   [ft][2 CT K-steps][parts] blocks, lane (h, l32), value i:
+//         w(16 st + 8 h + i, 32 ft + l32)
+//   down: [ft][CT][2 K-steps][parts] blocks: w(32 ct + l32, 32 ft + acc_krow(q, h, i))
+// fp32 problems: in two fp16 parts of w 2^-e, e[ft] stored.
+struct PackArgs {
+  const void* W[5];
+  u32x4* out[5];
+  int* e[5];
+  int sc[5], sf[5], down[5];
+  int n;
+};
+
+template <bool BF>
+__global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a, int C, int F, int CT) {
+  extern __shared__ float tile[];  // [32][32 CT + 1]
+  __shared__ float red[4];
+  constexpr int P = BF ? 1 : 2;
+  const int ft = blockIdx.x, j = blockIdx.y, tid = threadIdx.x;
+  const int Cp = 32 * CT, ld = Cp + 1, sc = a.sc[j], sf = a.sf[j];
+  float mx = 0.f;
+  for (int i = tid; i < 32 * Cp; i += 256) {
+    // the index with stride 1 runs over the lanes
+    const int f = sf == 1 ? i & 31 : i / Cp, c = sf == 1 ? i >> 5 : i - (i / Cp) * Cp;
+    const bool ok = c < C && 32 * ft + f < F;
+    const size_t at = size_t(c) * sc + size_t(32 * ft + f) * sf;
+    float v = 0.f;
+    if (ok) v = BF ? bf16_to_f32(static_cast<const uint16_t*>(a.W[j])[at]) : static_cast<const float*>(a.W[j])[at];
+    tile[f * ld + c] = v;
+    mx = fmaxf(mx, fabsf(v));
+  }
+  float scale = 1.f;
+  if constexpr (!BF) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if ((tid & 63) == 0) red[tid >> 6] = mx;
+  }
+  __syncthreads();
+  if constexpr (!BF) {
+    const int e = f16_split_exponent(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+    scale = ldexpf(1.f, -e);
+    if (tid == 0) a.e[j][ft] = e;
+  }
+  u32x4* out = a.out[j] + size_t(ft) * 2 * CT * P * kBlk;
+  for (int i = tid; i < 2 * CT * kBlk; i += 256) {
+    const int blk = i / kBlk, ln = i & 63, h = ln >> 5, l32 = ln & 31;
+    u32x4 w[P];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        v[u] = a.down[j] ? tile[acc_krow(blk & 1, h, 2 * k + u) * ld + 32 * (blk >> 1) + l32]
+                         : tile[l32 * ld + 16 * blk + 8 * h + 2 * k + u];
+      if constexpr (BF) {
+        w[0][k] = pack_bf16x2_rne(v[0], v[1]);  // (exact: the values are bf16)
+      } else {
+        uint32_t hi, lo;
+        split_f16x2_pair(v[0] * scale, v[1] * scale, hi, lo);
+        w[0][k] = hi;
+        w[1][k] = lo;
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) out[(blk * P + p) * kBlk + ln] = w[p];
+  }
+}
+
+// --------------------------------------------------------------------- gate
+// s = act(q) and, if asked for, act'(q), [N, 32 FT] fp32 each: a wave takes 32
+// nodes (lanes) and kGateTiles tiles of hidden units.
+constexpr int kGateTiles = 2;
+template <int CT, bool BF>
+__global__ __launch_bounds__(256) void k_ffn_gate(int N, int d, int C, int F, int FT, int act,
+                                                  const void* __restrict__ x, const u32x4* __restrict__ wg,
+                                                  const int* __restrict__ eg, const float* __restrict__ b,
+                                                  float* __restrict__ s, float* __restrict__ ds) {
+  constexpr int P = BF ? 1 : 2;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, l32 = lane & 31;
+  const int n = (blockIdx.x * 4 + wave) * kTile + l32;
+  if (n - l32 >= N) return;
+  u32x4 xo[2 * CT][P];
+  const int ex = load_row<CT, BF>(x, n < N, n < N ? size_t(n) * d * C : 0, C, h, xo);
+  for (int ft = blockIdx.y * kGateTiles; ft < min(FT, int(blockIdx.y + 1) * kGateTiles); ++ft) {
+    f32x16 acc = f32x16{};
+    const u32x4* w = wg + size_t(ft) * 2 * CT * P * kBlk + lane;
+#pragma unroll
+    for (int st = 0; st < 2 * CT; ++st) {
+      u32x4 a[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) a[p] = w[(st * P + p) * kBlk];
+      acc = mm_parts<BF>(a, xo[st], acc);
+    }
+    const int e = BF ? 0 : ex + eg[ft];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int f = 32 * ft + 8 * k + 4 * h;
+      f32x4 sv = f32x4{}, dv = f32x4{};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (f < F) {  // (F is a multiple of 16: a quad is inside or outside)
+          float s1, d1;
+          gate_act((BF ? acc[4 * k + i] : ldexpf(acc[4 * k + i], e)) + (b ? b[f + i] : 0.f), act, s1, d1);
+          sv[i] = s1;
+          dv[i] = d1;
+        }
+      if (n < N) {
+        *reinterpret_cast<f32x4*>(s + size_t(n) * 32 * FT + f) = sv;
+        if (ds) *reinterpret_cast<f32x4*>(ds + size_t(n) * 32 * FT + f) = dv;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------ forward and grad_x
+struct RowsArgs {
+  int M, d, C, FT;
+  const void* in;            // [M, C]
+  const u32x4 *up, *down;    // packed weights
+  const int *e_up, *e_down;  // their exponents (fp32 problems)
+  const float* s;            // [M / d, 32 FT]
+  const void* residual;      // [M, C] of the problem's type, or nullptr
+  const float* residual0;    // [M / d, C], added to the degree-0 rows, or nullptr
+  void* out;                 // [M, C]
+};
+
+// A workgroup takes 4 x 32 NB rows.  The packed weights of one tile of F come
+// into LDS by direct loads while the tile before is used.
+template <int CT, bool BF, int NB>
+__global__ __launch_bounds__(256) void k_ffn_rows(RowsArgs a) {
+  constexpr int P = BF ? 1 : 2;
+  constexpr int kHalf = 2 * CT * P * kBlk;  // words of a tile's up (and down) operands
+  extern __shared__ u32x4 sw[];             // [2][2 kHalf]
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int C = a.C, FT = a.FT;
+  auto fetch = [&](int ft, int buf) {
+#pragma unroll
+    for (int k = 0; k < CT * P; ++k) {
+      const int blk = wave * CT * P + k;  // of 4 CT P: the up operands, then the down operands
+      const u32x4* src = (blk < 2 * CT * P ? a.up + size_t(ft) * kHalf + blk * kBlk
+                                           : a.down + size_t(ft) * kHalf + (blk - 2 * CT * P) * kBlk) + lane;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)src,
+          (__attribute__((address_space(3))) void*)(sw + buf * 2 * kHalf + blk * kBlk), 16, 0, 0);
+    }
+  };
+  fetch(0, 0);
+  int row[NB], ex[NB], E[NB];
+  const float* s[NB];
+  u32x4 xo[NB][2 * CT][P];
+  f32x16 y[NB][CT];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    row[b] = (blockIdx.x * 4 + wave) * (kTile * NB) + b * kTile + l32;
+    const bool on = row[b] < a.M;
+    const int r = on ? row[b] : a.M - 1;
+    ex[b] = load_row<CT, BF>(a.in, on, size_t(r) * C, C, h, xo[b]);
+    s[b] = a.s + size_t(r / a.d) * 32 * FT + 4 * h;
+    E[b] = kUnset;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) y[b][ct] = f32x16{};
+  }
+  for (int ft = 0; ft < FT; ++ft) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share of the tile's weights is in LDS
+    __syncthreads();                     // every wave's is; the other buffer is free
+    if (ft + 1 < FT) fetch(ft + 1, (ft + 1) & 1);
+    const u32x4* w = sw + (ft & 1) * 2 * kHalf + lane;
+    f32x4 sv[NB][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 32 * ft + 8 * k);
+    f32x16 u[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) u[b] = f32x16{};
+#pragma unroll
+    for (int st = 0; st < 2 * CT; ++st) {
+      u32x4 wa[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) wa[p] = w[(st * P + p) * kBlk];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) u[b] = mm_parts<BF>(wa, xo[b][st], u[b]);
+    }
+    u32x4 ho[NB][2][P];
+    const int bias = BF ? 0 : a.e_up[ft] + a.e_down[ft];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      float t[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) t[v] = u[b][v] * sv[b][v >> 2][v & 3];
+      to_operand<BF>(t, bias, E[b], ho[b], [&](float f) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) y[b][ct] *= f;
+      });
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x4 wa[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) wa[p] = w[kHalf + ((2 * ct + q) * P + p) * kBlk];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) y[b][ct] = mm_parts<BF>(wa, ho[b][q], y[b][ct]);
+      }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    if (row[b] >= a.M) continue;
+    const int e = BF ? 0 : E[b] + ex[b];
+    const int n = row[b] / a.d;
+    const bool first = a.residual0 && n * a.d == row[b];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = 32 * ct + 8 * k + 4 * h;
+        if (c >= C) continue;
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = BF ? y[b][ct][4 * k + i] : ldexpf(y[b][ct][4 * k + i], e);
+        if (a.residual) v += load4<BF>(a.residual, size_t(row[b]) * C + c);
+        if (first) v += *reinterpret_cast<const f32x4*>(a.residual0 + size_t(n) * C + c);
+        store4<BF>(a.out, size_t(row[b]) * C + c, v);
+      }
+  }
+}
+
+// ------------------------------------------------------ the gate's gradients
+// r0 = dq W_gate^T [N, C]: a workgroup takes 32 nodes, each wave every fourth
+// tile of channels.
+template <int CT, bool BF>
+__global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const float* __restrict__ dq,
+                                                 const u32x4* __restrict__ wg, const int* __restrict__ eg,
+                                                 float* __restrict__ r0) {
+  constexpr int P = BF ? 1 : 2;
+  constexpr int T = (CT + 3) / 4;
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = blockIdx.x * kTile + l32;
+  const float* q = dq + size_t(min(n, N - 1)) * 32 * FT + 4 * h;
+  f32x16 acc[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) acc[t] = f32x16{};
+  int E = kUnset;
+  for (int ft = 0; ft < FT; ++ft) {
+    float t[16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(q + 32 * ft + 8 * k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t[4 * k + i] = v[i];
+    }
+    u32x4 o[2][P];
+    to_operand<BF>(t, BF ? 0 : eg[ft], E, o, [&](float f) {
+#pragma unroll
+      for (int j = 0; j < T; ++j) acc[j] *= f;
+    });
+#pragma unroll
+    for (int j = 0; j < T; ++j) {
+      const int ct = wave + 4 * j;
+      if (ct >= CT) break;
+#pragma unroll
+      for (int qq = 0; qq < 2; ++qq) {
+        u32x4 w[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) w[p] = wg[((size_t(ft) * CT + ct) * 2 + qq) * P * kBlk + p * kBlk + lane];
+        acc[j] = mm_parts<BF>(w, o[qq], acc[j]);
+      }
+    }
+  }
+  if (n >= N) return;
+#pragma unroll
+  for (int j = 0; j < T; ++j) {
+    const int ct = wave + 4 * j;
+    if (ct >= CT) break;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = 32 * ct + 8 * k + 4 * h;
+      if (c >= C) continue;
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = BF ? acc[j][4 * k + i] : ldexpf(acc[j][4 * k + i], E);
+      *reinterpret_cast<f32x4*>(r0 + size_t(n) * C + c) = v;
+    }
+  }
+}
+
+// grad W_gate = x[:, 0]^T dq in 32x32x2 fp32 MFMA, one tile of 32 x 32 a wave
+// over a range of nodes; the waves of the first channel tile also sum dq
+// (grad b).  partial [S][C + 1][32 FT]: the last row is grad b.
+template <bool BF>
+__global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, int FT, const void* __restrict__ x,
+                                                 const float* __restrict__ dq, float* __restrict__ partial) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, l32 = lane & 31;
+  const int t = blockIdx.x * 4 + wave;
+  if (t >= CT * FT) return;
+  const int ct = t / FT, ft = t - ct * FT, c = 32 * ct + l32, f = 32 * ft + l32;
+  const int n0 = int(int64_t(blockIdx.y) * N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * N / gridDim.y);
+  f32x16 acc = f32x16{};
+  float sum = 0.f;
+  auto at = [&](int n) {
+    if constexpr (BF)
+      return bf16_to_f32(static_cast<const uint16_t*>(x)[size_t(n) * d * C + c]);
+    else
+      return static_cast<const float*>(x)[size_t(n) * d * C + c];
+  };
+  for (int n = n0; n < n1; n += 16) {
+    float av[8], bv[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int nn = n + 2 * k + h;
+      av[k] = nn < n1 && c < C ? at(nn) : 0.f;
+      bv[k] = nn < n1 ? dq[size_t(nn) * 32 * FT + f] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      acc = mfma32(av[k], bv[k], acc);
+      sum += bv[k];
+    }
+  }
+  float* out = partial + size_t(blockIdx.y) * (C + 1) * 32 * FT + f;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    const int cc = 32 * ct + acc_row(v, h);
+    if (cc < C) out[size_t(cc) * 32 * FT] = acc[v];
+  }
+  sum += other_half(sum);
+  if (ct == 0 && h == 0) out[size_t(C) * 32 * FT] = sum;
+}
+
+// ------------------------------------------------------- weights' gradients
+struct WgradArgs {
+  int N, d, C, FT;
+  const void *x, *gy;             // [N d, C]
+  const u32x4 *up_u, *up_d;       // W_up and W_down^T packed as `up`
+  const int *e_u, *e_d;
+  const float *s, *ds;            // act(q), act'(q) [N, 32 FT]
+  float* dq;                      // [N, 32 FT]
+  float* partial;                 // [gridDim.y][2][C][32 FT]: W_down's (as [c][f]), then W_up's
+};
+
+// hidden tiles per pair of waves: what 512 registers hold
+__host__ __device__ constexpr int wgrad_tiles(int CT, bool BF) { return BF || CT <= 4 ? 2 : 1; }
+// LDS words: x and grad_y in both operand orders, then u and p of the pairs
+__host__ __device__ constexpr int wgrad_words(int CT, bool BF) {
+  return 4 * 2 * CT * (BF ? 1 : 2) * kBlk + 2 * 2 * wgrad_tiles(CT, BF) * 4 * kBlk;
+}
+
+template <int CT, bool BF>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_ffn_wgrad(WgradArgs a) {
+  constexpr int P = BF ? 1 : 2, NF = wgrad_tiles(CT, BF);
+  constexpr int kOp = 2 * CT * P * kBlk;
+  constexpr int kItems = (64 * CT + 255) / 256;  // 4 x 4 blocks of a 32-row tile per thread and tensor
+  extern __shared__ u32x4 smem[];
+  __shared__ uint32_t s_max[2][32];
+  __shared__ float s_rowf[32];
+  __shared__ int s_eb;
+  u32x4* sU = smem + 4 * kOp;                                      // [pair][NF][4][64]
+  float* sP = reinterpret_cast<float*>(sU + 2 * NF * 4 * kBlk);     // [pair][NF][32 rows][32]
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int role = wave & 1, g = wave >> 1;  // role 0: u and grad W_down; 1: dh and grad W_up
+  const int C = a.C, d = a.d, FT = a.FT, Fp = 32 * FT;
+  const int n0 = int(int64_t(blockIdx.y) * a.N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * a.N / gridDim.y);
+  const int r0 = n0 * d, r1 = n1 * d;
+  // a pair without a tile of its own repeats the last one and stores nothing
+  int ft[NF];
+  bool own[NF];
+  u32x4 w[NF][2 * CT][P];
+  int ew[NF], e_other[NF];
+#pragma unroll
+  for (int j = 0; j < NF; ++j) {
+    const int t = (blockIdx.x * 2 + g) * NF + j;
+    own[j] = t < FT;
+    ft[j] = min(t, FT - 1);
+    const u32x4* src = (role == 0 ? a.up_u : a.up_d) + size_t(ft[j]) * kOp + lane;
+#pragma unroll
+    for (int st = 0; st < 2 * CT; ++st)
+#pragma unroll
+      for (int p = 0; p < P; ++p) w[j][st][p] = src[(st * P + p) * kBlk];
+    ew[j] = BF ? 0 : (role == 0 ? a.e_u : a.e_d)[ft[j]];
+    e_other[j] = BF ? 0 : (role == 0 ? a.e_d : a.e_u)[ft[j]];
+  }
+  // LDS: x in row order, x in transposed order, then grad_y in both
+  const u32x4* rows_op = smem + (role == 0 ? 0 : 2) * kOp + lane;  // x for u, grad_y for dh
+  const u32x4* cols_op = smem + (role == 0 ? 3 : 1) * kOp + lane;  // grad_y for W_down, x for W_up
+  f32x16 acc[NF][CT];
+  int E[NF];
+#pragma unroll
+  for (int j = 0; j < NF; ++j) {
+    E[j] = kUnset;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) acc[j][ct] = f32x16{};
+  }
+  // this lane's running sum over a node's rows (waves of role 0: one lane a
+  // hidden unit of the pair's tiles), and the row's place in its node
+  float run = 0.f;
+  int in_node = 0, node = n0;
+  const int sum_j = NF == 2 ? lane >> 5 : 0;
+  const bool sums = role == 0 && (NF == 2 || h == 0) && (blockIdx.x * 2 + g) * NF + sum_j < FT;
+  const int sum_f = 32 * min((int(blockIdx.x) * 2 + g) * NF + sum_j, FT - 1) + l32;
+  auto add_rows = [&](int n) {  // the first n rows of sP
+    for (int r = 0; r < n; ++r) {
+      run += sP[((g * NF + sum_j) * 32 + r) * 32 + l32];
+      if (++in_node == d) {
+        if (sums) a.dq[size_t(node) * Fp + sum_f] = run * a.ds[size_t(node) * Fp + sum_f];
+        run = 0.f;
+        in_node = 0;
+        ++node;
+      }
+    }
+  };
+  f32x4 vx[kItems][4], vg[kItems][4];
+  auto fetch = [&](int rb) {
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int i = tid + 256 * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = rb + 4 * rg + r;
+        const bool on = i < 64 * CT && c < C && row < r1;
+        vx[k][r] = on ? load4<BF>(a.x, size_t(row) * C + c) : f32x4{};
+        vg[k][r] = on ? load4<BF>(a.gy, size_t(row) * C + c) : f32x4{};
+      }
+    }
+  };
+  // a 4 x 4 block into both operand orders
+  auto put = [&](const f32x4 (&v)[4], int rg, int c, u32x4* op, const float* sc) {
+    uint32_t hl[P][4][2];  // [part][row][pair of channels]
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if constexpr (BF)
+          hl[0][r][k] = pack_bf16x2_rne(v[r][2 * k], v[r][2 * k + 1]);
+        else
+          split_f16x2_pair(v[r][2 * k] * sc[r], v[r][2 * k + 1] * sc[r], hl[0][r][k], hl[1][r][k]);
+      }
+    const int st = c >> 4, hh = (c >> 3) & 1;
+    const int ct = c >> 5, q = rg >> 2, ht = rg & 1, it = (rg >> 1) & 1;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        reinterpret_cast<uint2*>(op + (st * P + p) * kBlk + hh * 32 + 4 * rg + r)[(c >> 2) & 1] =
+            uint2{hl[p][r][0], hl[p][r][1]};
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) {
+        const int k = cc >> 1, sh = 16 * (cc & 1);
+        const uint32_t lo = ((hl[p][0][k] >> sh) & 0xffffu) | ((hl[p][1][k] >> sh) << 16);
+        const uint32_t hi = ((hl[p][2][k] >> sh) & 0xffffu) | ((hl[p][3][k] >> sh) << 16);
+        reinterpret_cast<uint2*>(op + kOp + ((2 * ct + q) * P + p) * kBlk + ht * 32 + ((c + cc) & 31))[it] =
+            uint2{lo, hi};
+      }
+    }
+  };
+  if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
+  fetch(r0);
+  int prev = 0;  // rows of the tile before, whose products wait in sP
+  for (int rb = r0; rb < r1; rb += 32) {
+    __syncthreads();  // s_max is zero; the tile before is consumed
+    if constexpr (!BF) {
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) {
+        const int i = tid + 256 * k, rg = i / (8 * CT);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float mx = 0.f, mg = 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            mx = fmaxf(mx, fabsf(vx[k][r][c]));
+            mg = fmaxf(mg, fabsf(vg[k][r][c]));
+          }
+#pragma unroll
+          for (int o = 4; o > 0; o >>= 1) {
+            mx = fmaxf(mx, __shfl_xor(mx, o));
+            mg = fmaxf(mg, __shfl_xor(mg, o));
+          }
+          if ((lane & 7) == 0 && i < 64 * CT) {
+            atomicMax(&s_max[0][4 * rg + r], __float_as_uint(mx));
+            atomicMax(&s_max[1][4 * rg + r], __float_as_uint(mg));
+          }
+        }
+      }
+      __syncthreads();
+      if (tid < 64) {
+        // 2^(e_x + e_gy) of each row, relative to the largest of the tile's
+        const float mx = __uint_as_float(s_max[0][l32]), mg = __uint_as_float(s_max[1][l32]);
+        const int e = mx > 0.f && mg > 0.f ? f16_split_exponent(mx) + f16_split_exponent(mg) : kUnset;
+        int top = e;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o));
+        if (tid < 32) s_rowf[l32] = ldexpf(1.f, e - top);
+        if (tid == 0) s_eb = top;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int i = tid + 256 * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
+      if (i < 64 * CT) {
+        float sx[4], sg[4];
+        if constexpr (!BF) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            sx[r] = ldexpf(1.f, -f16_split_exponent(__uint_as_float(s_max[0][4 * rg + r])));
+            sg[r] = ldexpf(1.f, -f16_split_exponent(__uint_as_float(s_max[1][4 * rg + r])));
+          }
+        }
+        put(vx[k], rg, c, smem, sx);
+        put(vg[k], rg, c, smem + 2 * kOp, sg);
+      }
+    }
+    __syncthreads();
+    if (rb + 32 < r1) fetch(rb + 32);
+    if constexpr (!BF)
+      if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
+    // u or dh of the tile: rows in registers, hidden units in lanes
+    f32x16 t[NF];
+#pragma unroll
+    for (int j = 0; j < NF; ++j) t[j] = f32x16{};
+#pragma unroll
+    for (int st = 0; st < 2 * CT; ++st) {
+      u32x4 op[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) op[p] = rows_op[(st * P + p) * kBlk];
+#pragma unroll
+      for (int j = 0; j < NF; ++j) t[j] = mm_parts<BF>(op, w[j][st], t[j]);
+    }
+    if (role == 0) {
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          sU[((g * NF + j) * 4 + k) * kBlk + lane] =
+              __builtin_bit_cast(u32x4, f32x4{t[j][4 * k], t[j][4 * k + 1], t[j][4 * k + 2], t[j][4 * k + 3]});
+      add_rows(prev);
+    }
+    prev = min(32, r1 - rb);
+    __syncthreads();
+    const int eb = BF ? 0 : s_eb;
+    float rowf[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) rowf[v] = BF ? 1.f : s_rowf[acc_row(v, h)];
+    u32x4 o[NF][2][P];
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      if (role == 1) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const f32x4 u = __builtin_bit_cast(f32x4, sU[((g * NF + j) * 4 + k) * kBlk + lane]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = u[i] * rowf[4 * k + i] * t[j][4 * k + i];
+            sP[((g * NF + j) * 32 + acc_row(4 * k + i, h)) * 32 + l32] = BF ? p : ldexpf(p, eb + ew[j] + e_other[j]);
+          }
+        }
+      }
+      float v16[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int row = min(rb + acc_row(v, h), r1 - 1);
+        v16[v] = t[j][v] * rowf[v] * a.s[size_t(row / d) * Fp + 32 * ft[j] + l32];
+      }
+      to_operand<BF>(v16, eb, E[j], o[j], [&](float f) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) acc[j][ct] *= f;
+      });
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x4 op[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) op[p] = cols_op[((2 * ct + q) * P + p) * kBlk];
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[j][ct] = mm_parts<BF>(op, o[j][q], acc[j][ct]);
+      }
+  }
+  __syncthreads();
+  if (role == 0) add_rows(prev);
+#pragma unroll
+  for (int j = 0; j < NF; ++j) {
+    if (!own[j]) continue;
+    float* out = a.partial + (size_t(blockIdx.y) * 2 + role) * C * Fp + 32 * ft[j] + l32;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int c = 32 * ct + acc_row(v, h);
+        if (c < C) out[size_t(c) * Fp] = BF ? acc[j][ct][v] : ldexpf(acc[j][ct][v], E[j] + ew[j]);
+      }
+  }
+}
+
+// The ranges' sums in range order: a workgroup takes a 32 x 32 tile of one of
+// W_down's (z = 0, transposed on the way), W_up's (1) or W_gate's (2)
+// gradient; with z = 2 the first channel tile also takes grad b.
+template <bool BF>
+__global__ __launch_bounds__(256) void k_ffn_wsum(int C, int F, int FT, int S, int Sg,
+                                                  const float* __restrict__ partial,
+                                                  const float* __restrict__ partial_g, void* __restrict__ gd,
+                                                  void* __restrict__ gu, void* __restrict__ gg,
+                                                  float* __restrict__ gb) {
+  __shared__ float tile[32][33];
+  const int Fp = 32 * FT, c0 = 32 * blockIdx.y, f0 = 32 * blockIdx.x, z = blockIdx.z;
+  const int col = threadIdx.x & 31, r8 = threadIdx.x >> 5;
+  void* out = z == 0 ? gd : (z == 1 ? gu : gg);
+  auto put = [&](size_t i, float v) {
+    if constexpr (BF)
+      static_cast<uint16_t*>(out)[i] = uint16_t(pack_bf16x2_rne(v, 0.f));
+    else
+      static_cast<float*>(out)[i] = v;
+  };
+  const float* src = z < 2 ? partial + size_t(z) * C * Fp : partial_g;
+  const size_t step = z < 2 ? size_t(2) * C * Fp : size_t(C + 1) * Fp;
+  const int n = z < 2 ? S : Sg;
+  if (out) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + r8 + 8 * k, f = f0 + col;
+      float v = 0.f;
+      if (c < C)
+        for (int p = 0; p < n; ++p) v += src[p * step + size_t(c) * Fp + f];
+      if (z == 0)
+        tile[r8 + 8 * k][col] = v;
+      else if (c < C && f < F)
+        put(size_t(c) * F + f, v);
+    }
+    if (z == 0) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = c0 + col, f = f0 + r8 + 8 * k;
+        if (c < C && f < F) put(size_t(f) * C + c, tile[col][r8 + 8 * k]);
+      }
+    }
+  }
+  if (z == 2 && gb && blockIdx.y == 0 && r8 == 0 && f0 + col < F) {
+    float v = 0.f;
+    for (int p = 0; p < n; ++p) v += src[p * step + size_t(C) * Fp + f0 + col];
+    gb[f0 + col] = v;
+  }
+}
+
+size_t al256(size_t b) { return (b + 255) & ~size_t(255); }
+
+struct Layout {
+  size_t pack[5], exps, s, ds, dq, r0, part, part_g, total;
+  int CT, FT, P, S, Sg;
+  size_t pack_bytes;
+};
+// packs: up, down, gate (forward); W_up and W_down^T as up, W_up^T as down,
+// gate, W_gate^T as down (backward)
+Layout layout(const FfnShape& p, bool backward) {
+  Layout l{};
+  l.CT = (p.C + 31) / 32;
+  l.FT = (p.F + 31) / 32;
+  l.P = p.bf16 ? 1 : 2;
+  l.pack_bytes = size_t(l.FT) * 2 * l.CT * l.P * kBlk * 16;
+  size_t o = 0;
+  for (int j = 0; j < (backward ? 5 : 3); ++j) {
+    l.pack[j] = o;
+    o += al256(l.pack_bytes);
+  }
+  l.exps = o;
+  o += al256(size_t(5) * l.FT * 4);
+  const size_t gate = al256(size_t(p.N) * 32 * l.FT * 4);
+  l.s = o;
+  o += gate;
+  if (backward) {
+    l.ds = o;
+    o += gate;
+    l.dq = o;
+    o += gate;
+    l.r0 = o;
+    o += al256(size_t(p.N) * p.C * 4);
+    // one workgroup a CU over the ranges of rows; a range has a node at least
+    const int per = 2 * wgrad_tiles(l.CT, p.bf16), fb = (l.FT + per - 1) / per;
+    const int most = device_cus() / fb;
+    l.S = p.N < most ? p.N : (most > 1 ? most : 1);
+    if (l.S < 1) l.S = 1;
+    l.part = o;
+    o += al256(size_t(l.S) * 2 * p.C * 32 * l.FT * 4);
+    const int blocks = (l.CT * l.FT + 3) / 4;
+    int sg = 2 * device_cus() / blocks;
+    const int cap = (p.N + 63) / 64;  // at least 64 nodes a range
+    l.Sg = sg < cap ? sg : cap;
+    if (l.Sg < 1) l.Sg = 1;
+    l.part_g = o;
+    o += al256(size_t(l.Sg) * (p.C + 1) * 32 * l.FT * 4);
+  }
+  l.total = o;
+  return l;
+}
+
+void add_pack(PackArgs& a, const Layout& l, char* ws, int slot, const void* W, int sc, int sf, int down) {
+  const int j = a.n++;
+  a.W[j] = W;
+  a.out[j] = reinterpret_cast<u32x4*>(ws + l.pack[slot]);
+  a.e[j] = reinterpret_cast<int*>(ws + l.exps) + slot * l.FT;
+  a.sc[j] = sc;
+  a.sf[j] = sf;
+  a.down[j] = down;
+}
+
+template <bool BF>
+hipError_t pack(const PackArgs& a, const Layout& l, const FfnShape& p, hipStream_t s) {
+  const size_t lds = size_t(32) * (32 * l.CT + 1) * 4;
+  k_ffn_pack<BF><<<dim3(l.FT, a.n), dim3(256), lds, s>>>(a, p.C, p.F, l.CT);
+  return hipGetLastError();
+}
+
+template <int CT, bool BF>
+hipError_t gate(const Layout& l, const FfnShape& p, const void* x, char* ws, int slot, const float* b, bool slope,
+                hipStream_t s) {
+  const dim3 grid((p.N + 127) / 128, (l.FT + kGateTiles - 1) / kGateTiles);
+  k_ffn_gate<CT, BF><<<grid, dim3(256), 0, s>>>(
+      p.N, p.d, p.C, p.F, l.FT, p.act, x, reinterpret_cast<const u32x4*>(ws + l.pack[slot]),
+      reinterpret_cast<const int*>(ws + l.exps) + slot * l.FT, b, reinterpret_cast<float*>(ws + l.s),
+      slope ? reinterpret_cast<float*>(ws + l.ds) : nullptr);
+  return hipGetLastError();
+}
+
+template <int CT, bool BF, int NB>
+hipError_t rows_nb(const RowsArgs& a, hipStream_t s) {
+  const size_t lds = size_t(2) * 4 * CT * (BF ? 1 : 2) * kBlk * 16;
+  auto k = k_ffn_rows<CT, BF, NB>;
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+  if (e != hipSuccess) return e;
+  k<<<dim3((a.M + 128 * NB - 1) / (128 * NB)), dim3(256), lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int CT, bool BF>
+hipError_t rows(const RowsArgs& a, hipStream_t s) {
+  return rows_nb<CT, BF, 1>(a, s);
+}
+
+template <int CT, bool BF>
+hipError_t forward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
+  const Layout l = layout(p, false);
+  char* ws = static_cast<char*>(a.ws);
+  PackArgs pk{};
+  add_pack(pk, l, ws, 0, a.w_up, p.F, 1, 0);
+  add_pack(pk, l, ws, 1, a.w_down, 1, p.C, 1);
+  add_pack(pk, l, ws, 2, a.w_gate, p.F, 1, 0);
+  hipError_t e = pack<BF>(pk, l, p, s);
+  if (e == hipSuccess) e = gate<CT, BF>(l, p, a.x, ws, 2, a.b_gate, false, s);
+  if (e != hipSuccess) return e;
+  const int* ex = reinterpret_cast<const int*>(ws + l.exps);
+  RowsArgs r{};
+  r.M = p.N * p.d;
+  r.d = p.d;
+  r.C = p.C;
+  r.FT = l.FT;
+  r.in = a.x;
+  r.up = reinterpret_cast<const u32x4*>(ws + l.pack[0]);
+  r.down = reinterpret_cast<const u32x4*>(ws + l.pack[1]);
+  r.e_up = ex;
+  r.e_down = ex + l.FT;
+  r.s = reinterpret_cast<const float*>(ws + l.s);
+  r.residual = a.residual;
+  r.out = a.y;
+  return rows<CT, BF>(r, s);
+}
+
+template <int CT, bool BF>
+hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
+  const Layout l = layout(p, true);
+  char* ws = static_cast<char*>(a.ws);
+  PackArgs pk{};
+  add_pack(pk, l, ws, 0, a.w_up, p.F, 1, 0);
+  add_pack(pk, l, ws, 1, a.w_down, 1, p.C, 0);
+  add_pack(pk, l, ws, 2, a.w_up, p.F, 1, 1);
+  add_pack(pk, l, ws, 3, a.w_gate, p.F, 1, 0);
+  add_pack(pk, l, ws, 4, a.w_gate, p.F, 1, 1);
+  hipError_t e = pack<BF>(pk, l, p, s);
+  if (e == hipSuccess) e = gate<CT, BF>(l, p, a.x, ws, 3, a.b_gate, true, s);
+  if (e != hipSuccess) return e;
+  const int* ex = reinterpret_cast<const int*>(ws + l.exps);
+  float* dq = reinterpret_cast<float*>(ws + l.dq);
+  WgradArgs w{};
+  w.N = p.N;
+  w.d = p.d;
+  w.C = p.C;
+  w.FT = l.FT;
+  w.x = a.x;
+  w.gy = a.grad_y;
+  w.up_u = reinterpret_cast<const u32x4*>(ws + l.pack[0]);
+  w.up_d = reinterpret_cast<const u32x4*>(ws + l.pack[1]);
+  w.e_u = ex;
+  w.e_d = ex + l.FT;
+  w.s = reinterpret_cast<const float*>(ws + l.s);
+  w.ds = reinterpret_cast<const float*>(ws + l.ds);
+  w.dq = dq;
+  w.partial = reinterpret_cast<float*>(ws + l.part);
+  {
+    const size_t lds = size_t(wgrad_words(CT, BF)) * 16;
+    auto k = k_ffn_wgrad<CT, BF>;
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+    if (e != hipSuccess) return e;
+    const int per = 2 * wgrad_tiles(CT, BF);
+    k<<<dim3((l.FT + per - 1) / per, l.S), dim3(256), lds, s>>>(w);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  float* part_g = reinterpret_cast<float*>(ws + l.part_g);
+  if (a.grad_w_gate || a.grad_b_gate) {
+    k_ffn_dwg<BF><<<dim3((l.CT * l.FT + 3) / 4, l.Sg), dim3(256), 0, s>>>(p.N, p.d, p.C, l.CT, l.FT, a.x, dq, part_g);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.grad_w_up || a.grad_w_down || a.grad_w_gate || a.grad_b_gate) {
+    k_ffn_wsum<BF><<<dim3(l.FT, l.CT, 3), dim3(256), 0, s>>>(p.C, p.F, l.FT, l.S, l.Sg, w.partial, part_g,
+                                                             a.grad_w_down, a.grad_w_up, a.grad_w_gate, a.grad_b_gate);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!a.grad_x) return hipSuccess;
+  float* r0 = reinterpret_cast<float*>(ws + l.r0);
+  k_ffn_dx0<CT, BF><<<dim3((p.N + 31) / 32), dim3(256), 0, s>>>(
+      p.N, p.C, l.FT, dq, reinterpret_cast<const u32x4*>(ws + l.pack[4]), ex + 4 * l.FT, r0);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  RowsArgs r{};
+  r.M = p.N * p.d;
+  r.d = p.d;
+  r.C = p.C;
+  r.FT = l.FT;
+  r.in = a.grad_y;
+  r.up = w.up_d;
+  r.down = reinterpret_cast<const u32x4*>(ws + l.pack[2]);
+  r.e_up = ex + l.FT;
+  r.e_down = ex + 2 * l.FT;
+  r.s = w.s;
+  r.residual0 = r0;
+  r.out = a.grad_x;
+  return rows<CT, BF>(r, s);
+}
+
+template <bool BF>
+hipError_t dispatch(const FfnShape& p, const FfnArgs& a, bool back, hipStream_t s) {
+  switch ((p.C + 31) / 32) {
+#define TDN_FFN_CASE(CTV) \
+  case CTV: return back ? backward<CTV, BF>(p, a, s) : forward<CTV, BF>(p, a, s);
+    TDN_FFN_CASE(1)
+    TDN_FFN_CASE(2)
+    TDN_FFN_CASE(3)
+    TDN_FFN_CASE(4)
+    TDN_FFN_CASE(5)
+    TDN_FFN_CASE(6)
+    TDN_FFN_CASE(7)
+    TDN_FFN_CASE(8)
+#undef TDN_FFN_CASE
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+size_t gated_ffn_ws_bytes(const FfnShape& p, bool backward) { return layout(p, backward).total; }
+
+hipError_t launch_gated_ffn(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
+  if (p.N == 0) return hipSuccess;
+  return p.bf16 ? dispatch<true>(p, a, false, s) : dispatch<false>(p, a, false, s);
+}
+
+hipError_t launch_gated_ffn_bwd(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
+  if (p.N == 0) {
+    const size_t w = size_t(p.C) * p.F * (p.bf16 ? 2 : 4);
+    hipError_t e = hipSuccess;
+    for (void* g : {a.grad_w_up, a.grad_w_gate, a.grad_w_down})
+      if (g && e == hipSuccess) e = launch_zero(g, w, s);
+    if (a.grad_b_gate && e == hipSuccess) e = launch_zero(a.grad_b_gate, size_t(p.F) * 4, s);
+    return e;
+  }
+  return p.bf16 ? dispatch<true>(p, a, true, s) : dispatch<false>(p, a, true, s);
+}
+
+}  // namespace tdn

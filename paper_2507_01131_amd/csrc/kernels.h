@@ -313,6 +313,41 @@ int bwd_dst_cpad(int C, bool bf16);
 __host__ __device__ inline int bwd_direct_cpad(int C) { return C <= 64 ? 64 : (C <= 128 ? 128 : 256); }
 hipError_t launch_bwd_dst(const BwdDstArgs& a, bool x_bf16, hipStream_t s);
 
+// ---------------------------------------------------------------- layer norm
+// The equivariant layer norm (layer_norm.hip) of x [N, (L + 1)^2, C] (fp32 or
+// bf16, y and the gradients' tensors alike): gamma [L + 1, C], beta [C] or
+// nullptr.  C a multiple of 16, at most 256.
+hipError_t launch_layer_norm(int N, int L, int C, bool bf16, float eps, const void* x, const float* gamma,
+                             const float* beta, void* y, hipStream_t s);
+// workgroups of the backward: partial holds that many [L + 2, C] sums
+int layer_norm_parts(int N, int C);
+// grad_res (added to grad_x) and every output may be nullptr
+hipError_t launch_layer_norm_bwd(int N, int L, int C, bool bf16, float eps, const void* x, const float* gamma,
+                                 const void* grad_y, const void* grad_res, void* grad_x, float* grad_gamma,
+                                 float* grad_beta, float* partial, hipStream_t s);
+
+// ---------------------------------------------------------------- feed-forward
+// The gated feed-forward block (gated_ffn.hip).  C and F multiples of 16,
+// C <= 256.
+constexpr int kActSilu = 0, kActGelu = 1, kActSigmoid = 2;
+struct FfnShape {
+  int N, d, C, F, act;
+  bool bf16;  // type of every tensor but b_gate and its gradient (fp32)
+};
+struct FfnArgs {
+  const void *x, *w_up, *w_gate, *w_down;  // [N, d, C], [C, F], [C, F], [F, C]
+  const float* b_gate;                     // [F] or nullptr
+  const void* residual;                    // [N, d, C] or nullptr (forward)
+  void* y;                                 // forward
+  const void* grad_y;                      // backward; its outputs may be nullptr:
+  void *grad_x, *grad_w_up, *grad_w_gate, *grad_w_down;
+  float* grad_b_gate;
+  void* ws;  // gated_ffn_ws_bytes
+};
+size_t gated_ffn_ws_bytes(const FfnShape& p, bool backward);
+hipError_t launch_gated_ffn(const FfnShape& p, const FfnArgs& a, hipStream_t s);
+hipError_t launch_gated_ffn_bwd(const FfnShape& p, const FfnArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- misc
 // Rank chunks (ranks above 256, split into column ranges):
 // dst[row][j] = src[row][r0 + j] for a row-major [rows, R] src and [rows, n] dst

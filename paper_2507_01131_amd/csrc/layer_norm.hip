@@ -1,0 +1,335 @@
+// Equivariant layer norm and its backward.
+//
+// Per node and degree l (rows l^2 .. (l + 1)^2 - 1 of x [N, d, C]), with
+// xc = x less its mean over channels for l = 0 and xc = x for l > 0,
+//   r = 1 / sqrt(mean over (m, c) of xc^2 + eps),  xhat = xc r,
+//   y = gamma[l] xhat (+ beta for l = 0).
+// Backward, with w = gamma[l] grad_y and the means over the degree's (m, c):
+//   grad_x = r (w - [l = 0] mean(w) - xhat mean(w xhat)) (+ grad_res),
+//   grad_gamma[l, c] = sum over n, m of grad_y xhat,
+//   grad_beta[c] = sum over n of grad_y of degree 0.
+//
+// Bound by memory: each value is read once and written once.  G = C / 4 lanes
+// rounded up to a power of two take one node, a lane four channels of every
+// row (16-byte loads of fp32, 8-byte of bf16), so a degree's sums over rows
+// stay in a lane and cross G lanes at the end.  The degrees are independent
+// of each other; the backward gives each its own workgroups, so that one
+// degree's rows of x and grad_y are in registers at a time.  It recomputes
+// the statistics from the x that it reads anyway; with S = sum(w xc) and
+// Q = sum(xc^2) taken together, mean(w xhat) = r S / n needs no second pass
+// over the row.  The sums over nodes stay in a lane's registers over all of
+// its nodes, are added in LDS over the workgroup's groups and then over the
+// workgroups, each in a fixed order.  Statistics, sums and products are fp32;
+// a bf16 output is rounded once, when it is stored.
+#include "common.hpp"
+#include "kernels.h"
+
+namespace tdn {
+
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kMaxNormL = 6;
+
+template <bool BF>
+__device__ __forceinline__ f32x4 load4(const void* p, size_t i) {
+  if constexpr (BF) {
+    const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+    return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                 __uint_as_float(u.y & 0xffff0000u)};
+  } else {
+    return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+  }
+}
+template <bool BF>
+__device__ __forceinline__ void store4(void* p, size_t i, f32x4 v) {
+  if constexpr (BF)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =
+        uint2{pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
+  else
+    *reinterpret_cast<f32x4*>(static_cast<float*>(p) + i) = v;
+}
+// element i of a tensor of the problem's type
+template <bool BF>
+__device__ __forceinline__ const void* row_at(const void* p, size_t i) {
+  return static_cast<const char*>(p) + i * (BF ? 2 : 4);
+}
+template <bool BF>
+__device__ __forceinline__ void* row_at(void* p, size_t i) {
+  return static_cast<char*>(p) + i * (BF ? 2 : 4);
+}
+__device__ __forceinline__ float sum4(f32x4 v) { return (v[0] + v[1]) + (v[2] + v[3]); }
+__device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
+  return fmaf(a[3], b[3], fmaf(a[2], b[2], fmaf(a[1], b[1], a[0] * b[0])));
+}
+// sum over the G lanes of a node's group (G a power of two, uniform)
+__device__ __forceinline__ float group_sum(float v, int G) {
+  for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// One degree of one node.  `first` (uniform) is the element where the
+// workgroup's nodes start, `lane` the lane's offset from there (0 where the
+// lane is off: it takes part in its group's sums with zeros).
+template <int l, bool BF>
+__device__ __forceinline__ void fwd_degree(bool on, size_t first, uint32_t lane, int C, int c, int G, float eps,
+                                           const void* __restrict__ x, const float* __restrict__ gamma,
+                                           const float* __restrict__ beta, void* __restrict__ y) {
+  constexpr int R = 2 * l + 1;
+  const float inv_n = 1.f / float(R * C);
+  const size_t at = first + size_t(l * l) * C;
+  f32x4 v[R];
+#pragma unroll
+  for (int m = 0; m < R; ++m) v[m] = load4<BF>(row_at<BF>(x, at + size_t(m) * C), lane);
+  if (!on)
+#pragma unroll
+    for (int m = 0; m < R; ++m) v[m] = f32x4{};
+  if constexpr (l == 0) {
+    const float mean = group_sum(sum4(v[0]), G) * inv_n;
+    if (on) v[0] -= mean;
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int m = 0; m < R; ++m) q += dot4(v[m], v[m]);
+  q = group_sum(q, G);
+  if (!on) return;
+  const f32x4 g = *reinterpret_cast<const f32x4*>(gamma + l * C + c) * (1.f / sqrtf(q * inv_n + eps));
+#pragma unroll
+  for (int m = 0; m < R; ++m) {
+    f32x4 o = v[m] * g;
+    if (l == 0 && beta) o += *reinterpret_cast<const f32x4*>(beta + c);
+    store4<BF>(row_at<BF>(y, at + size_t(m) * C), lane, o);
+  }
+}
+
+template <int L, bool BF>
+__global__ __launch_bounds__(kNormThreads) void k_norm_fwd(int N, int C, int G, float eps, const void* __restrict__ x,
+                                                           const float* __restrict__ gamma,
+                                                           const float* __restrict__ beta, void* __restrict__ y) {
+  constexpr int d = (L + 1) * (L + 1);
+  const int per = kNormThreads / G, c = 4 * int(threadIdx.x % G);
+  const int64_t n0 = int64_t(blockIdx.x) * per;
+  const bool on = n0 + threadIdx.x / G < N && c < C;
+  const size_t first = size_t(n0) * d * C;
+  const uint32_t lane = on ? uint32_t(threadIdx.x / G) * d * C + c : 0;
+#define TDN_DEGREE(l) \
+  if constexpr (L >= l) fwd_degree<l, BF>(on, first, lane, C, c, G, eps, x, gamma, beta, y);
+  TDN_DEGREE(0)
+  TDN_DEGREE(1)
+  TDN_DEGREE(2)
+  TDN_DEGREE(3)
+  TDN_DEGREE(4)
+  TDN_DEGREE(5)
+  TDN_DEGREE(6)
+#undef TDN_DEGREE
+}
+
+// Degree l of node groups b, b + gridDim.x, ...: grad_x, and the workgroup's
+// sums of grad_gamma[l] (and, with l = 0, of grad_beta) into partial
+// [gridDim.x][L + 2][C], the last row grad_beta's.
+template <int l, bool BF>
+__device__ __forceinline__ void bwd_degree(int N, int d, int C, int G, float eps, const void* __restrict__ x,
+                                           const float* __restrict__ gamma, const void* __restrict__ grad_y,
+                                           const void* __restrict__ grad_res, void* __restrict__ grad_x,
+                                           float* __restrict__ partial, int L, f32x4* red) {
+  constexpr int R = 2 * l + 1;
+  const int tid = threadIdx.x, per = kNormThreads / G, c = 4 * (tid % G);
+  const bool in_c = c < C;
+  const float inv_n = 1.f / float(R * C);
+  const f32x4 g = in_c ? *reinterpret_cast<const f32x4*>(gamma + l * C + c) : f32x4{};
+  f32x4 sg = f32x4{}, sb = f32x4{};
+#pragma clang loop unroll(disable)
+  for (int64_t n0 = int64_t(blockIdx.x) * per; n0 < N; n0 += int64_t(gridDim.x) * per) {
+    const bool on = n0 + tid / G < N && in_c;
+    const size_t at = (size_t(n0) * d + l * l) * C;
+    const uint32_t lane = on ? uint32_t(tid / G) * d * C + c : 0;
+    f32x4 v[R], w[R];
+#pragma unroll
+    for (int m = 0; m < R; ++m) {
+      v[m] = load4<BF>(row_at<BF>(x, at + size_t(m) * C), lane);
+      w[m] = load4<BF>(row_at<BF>(grad_y, at + size_t(m) * C), lane);
+    }
+    if (!on)
+#pragma unroll
+      for (int m = 0; m < R; ++m) v[m] = w[m] = f32x4{};
+    if constexpr (l == 0) {
+      const float mean = group_sum(sum4(v[0]), G) * inv_n;
+      if (on) v[0] -= mean;
+      sb += w[0];
+    }
+    float q = 0.f, s = 0.f, sw = 0.f;
+#pragma unroll
+    for (int m = 0; m < R; ++m) {
+      q += dot4(v[m], v[m]);
+      s += dot4(w[m] * g, v[m]);
+    }
+    if constexpr (l == 0) sw = sum4(w[0] * g);
+    for (int o = G >> 1; o > 0; o >>= 1) {
+      q += __shfl_xor(q, o);
+      s += __shfl_xor(s, o);
+      if constexpr (l == 0) sw += __shfl_xor(sw, o);
+    }
+    const float r = 1.f / sqrtf(q * inv_n + eps);
+    const float k = r * r * s * inv_n;  // of xc: r mean(w xhat)
+    f32x4 acc = f32x4{};
+#pragma unroll
+    for (int m = 0; m < R; ++m) {
+      acc += w[m] * v[m];
+      if (on && grad_x) {
+        f32x4 o = w[m] * g - v[m] * k;
+        if constexpr (l == 0) o -= sw * inv_n;
+        o *= r;
+        if (grad_res) o += load4<BF>(row_at<BF>(grad_res, at + size_t(m) * C), lane);
+        store4<BF>(row_at<BF>(grad_x, at + size_t(m) * C), lane, o);
+      }
+    }
+    sg += acc * r;
+  }
+  if (!partial) return;
+#pragma unroll
+  for (int k = 0; k < (l == 0 ? 2 : 1); ++k) {
+    __syncthreads();
+    red[tid] = k == 0 ? sg : sb;
+    __syncthreads();
+    if (tid < G && in_c) {
+      f32x4 t = red[tid];
+      for (int p = 1; p < per; ++p) t += red[p * G + tid];
+      *reinterpret_cast<f32x4*>(partial + (size_t(blockIdx.x) * (L + 2) + (k == 0 ? l : L + 1)) * C + c) = t;
+    }
+  }
+}
+
+// The workgroups of one y take one degree, the largest first.
+template <int L, bool BF>
+__global__ __launch_bounds__(kNormThreads) void k_norm_bwd(int N, int C, int G, float eps, const void* __restrict__ x,
+                                                           const float* __restrict__ gamma,
+                                                           const void* __restrict__ grad_y,
+                                                           const void* __restrict__ grad_res, void* __restrict__ grad_x,
+                                                           float* __restrict__ partial) {
+  constexpr int d = (L + 1) * (L + 1);
+  __shared__ f32x4 red[kNormThreads];
+  switch (L - int(blockIdx.y)) {
+#define TDN_DEGREE(l)                                                                                              \
+  case l:                                                                                                          \
+    if constexpr (L >= l) bwd_degree<l, BF>(N, d, C, G, eps, x, gamma, grad_y, grad_res, grad_x, partial, L, red); \
+    break;
+    TDN_DEGREE(0)
+    TDN_DEGREE(1)
+    TDN_DEGREE(2)
+    TDN_DEGREE(3)
+    TDN_DEGREE(4)
+    TDN_DEGREE(5)
+    TDN_DEGREE(6)
+#undef TDN_DEGREE
+  }
+}
+
+// grad_gamma and grad_beta from the workgroups' sums: 64 columns a workgroup,
+// sixteen threads a column, each a strided share of the parts in order.
+__global__ __launch_bounds__(1024) void k_norm_sum(int n_part, int n, int n_gamma, const float* __restrict__ partial,
+                                                   float* __restrict__ grad_gamma, float* __restrict__ grad_beta) {
+  __shared__ float red[16][64];
+  const int col = threadIdx.x & 63, k = threadIdx.x >> 6, i = blockIdx.x * 64 + col;
+  float s = 0.f;
+  if (i < n)
+    for (int p = k; p < n_part; p += 16) s += partial[size_t(p) * n + i];
+  red[k][col] = s;
+  __syncthreads();
+  if (k == 0 && i < n) {
+    for (int j = 1; j < 16; ++j) s += red[j][col];
+    if (i < n_gamma) {
+      if (grad_gamma) grad_gamma[i] = s;
+    } else if (grad_beta) {
+      grad_beta[i - n_gamma] = s;
+    }
+  }
+}
+
+int norm_group(int C) {
+  int G = 4;
+  while (4 * G < C) G <<= 1;
+  return G;
+}
+
+template <int L>
+hipError_t fwd_l(int N, int C, bool bf16, float eps, const void* x, const float* gamma, const float* beta, void* y,
+                 hipStream_t s) {
+  const int G = norm_group(C);
+  const int64_t blocks = (int64_t(N) * G + kNormThreads - 1) / kNormThreads;
+  if (bf16)
+    k_norm_fwd<L, true><<<dim3(uint32_t(blocks)), dim3(kNormThreads), 0, s>>>(N, C, G, eps, x, gamma, beta, y);
+  else
+    k_norm_fwd<L, false><<<dim3(uint32_t(blocks)), dim3(kNormThreads), 0, s>>>(N, C, G, eps, x, gamma, beta, y);
+  return hipGetLastError();
+}
+
+template <int L>
+hipError_t bwd_l(int N, int C, bool bf16, float eps, const void* x, const float* gamma, const void* grad_y,
+                 const void* grad_res, void* grad_x, float* partial, int nb, hipStream_t s) {
+  const int G = norm_group(C);
+  if (bf16)
+    k_norm_bwd<L, true><<<dim3(nb, L + 1), dim3(kNormThreads), 0, s>>>(N, C, G, eps, x, gamma, grad_y, grad_res,
+                                                                      grad_x, partial);
+  else
+    k_norm_bwd<L, false><<<dim3(nb, L + 1), dim3(kNormThreads), 0, s>>>(N, C, G, eps, x, gamma, grad_y, grad_res,
+                                                                       grad_x, partial);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int layer_norm_parts(int N, int C) {
+  const int per = kNormThreads / norm_group(C);
+  const int blocks = (N + per - 1) / per, most = 4 * device_cus();
+  return blocks < most ? blocks : most;
+}
+
+hipError_t launch_layer_norm(int N, int L, int C, bool bf16, float eps, const void* x, const float* gamma,
+                             const float* beta, void* y, hipStream_t s) {
+  if (N == 0) return hipSuccess;
+  switch (L) {
+#define TDN_NORM_CASE(LV) \
+  case LV: return fwd_l<LV>(N, C, bf16, eps, x, gamma, beta, y, s);
+    TDN_NORM_CASE(0)
+    TDN_NORM_CASE(1)
+    TDN_NORM_CASE(2)
+    TDN_NORM_CASE(3)
+    TDN_NORM_CASE(4)
+    TDN_NORM_CASE(5)
+    TDN_NORM_CASE(6)
+#undef TDN_NORM_CASE
+    default: return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_layer_norm_bwd(int N, int L, int C, bool bf16, float eps, const void* x, const float* gamma,
+                                 const void* grad_y, const void* grad_res, void* grad_x, float* grad_gamma,
+                                 float* grad_beta, float* partial, hipStream_t s) {
+  const int nb = layer_norm_parts(N, C);
+  const bool sums = grad_gamma || grad_beta;
+  if (N > 0) {
+    hipError_t e;
+    switch (L) {
+#define TDN_NORM_CASE(LV)                                                                                      \
+  case LV:                                                                                                     \
+    e = bwd_l<LV>(N, C, bf16, eps, x, gamma, grad_y, grad_res, grad_x, sums ? partial : nullptr, nb, s); \
+    break;
+      TDN_NORM_CASE(0)
+      TDN_NORM_CASE(1)
+      TDN_NORM_CASE(2)
+      TDN_NORM_CASE(3)
+      TDN_NORM_CASE(4)
+      TDN_NORM_CASE(5)
+      TDN_NORM_CASE(6)
+#undef TDN_NORM_CASE
+      default: return hipErrorInvalidValue;
+    }
+    if (e != hipSuccess) return e;
+  }
+  if (!sums) return hipSuccess;
+  const int n = (L + 2) * C;
+  k_norm_sum<<<dim3((n + 63) / 64), dim3(1024), 0, s>>>(N > 0 ? nb : 0, n, (L + 1) * C, partial, grad_gamma, grad_beta);
+  return hipGetLastError();
+}
+
+}  // namespace tdn

@@ -1,0 +1,120 @@
+"""Host-side checks of the norm's and the feed-forward block's entry points:
+every refusal happens before any device is touched (no GPU needed)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2507_01131_amd as tdn
+
+FAKE = ctypes.c_void_p(0x1000)   # never dereferenced
+ODD = ctypes.c_void_p(0x1008)
+SHAPE, DTYPE, NULL, WORKSPACE, MISALIGNED = 2, 3, 1, 4, 14
+
+
+def _norm(N=10, L=2, C=32, dtype=0, eps=1e-5, **kw):
+    a = dict(x=FAKE, gamma=FAKE, beta=FAKE, y=FAKE)
+    a.update(kw)
+    return tdn.lib().tdn_layer_norm_forward(N, L, C, dtype, eps, a["x"], a["gamma"], a["beta"], a["y"], None)
+
+
+def _norm_bwd(N=10, L=2, C=32, dtype=0, eps=1e-5, nbytes=1 << 40, **kw):
+    a = dict(x=FAKE, gamma=FAKE, gy=FAKE, res=None, gx=FAKE, gg=FAKE, gb=FAKE, ws=FAKE)
+    a.update(kw)
+    return tdn.lib().tdn_layer_norm_backward(N, L, C, dtype, eps, a["x"], a["gamma"], a["gy"], a["res"], a["gx"],
+                                             a["gg"], a["gb"], a["ws"], nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(N=-1), SHAPE), (dict(L=-1), SHAPE), (dict(L=7), SHAPE), (dict(C=8), SHAPE), (dict(C=40), SHAPE),
+    (dict(C=272), SHAPE), (dict(N=(1 << 31) // 9), SHAPE), (dict(eps=0.0), SHAPE), (dict(eps=-1.0), SHAPE),
+    (dict(eps=float("nan")), SHAPE), (dict(eps=float("inf")), SHAPE), (dict(dtype=2), DTYPE), (dict(dtype=-1), DTYPE),
+    (dict(x=None), NULL), (dict(gamma=None), NULL), (dict(x=ODD), MISALIGNED), (dict(gamma=ODD), MISALIGNED)])
+def test_layer_norm_refusals(kw, status):
+    assert _norm(**kw) == status
+    assert _norm_bwd(**kw) == status
+
+
+def test_layer_norm_pointers_of_one_direction():
+    assert _norm(y=None) == NULL and _norm(y=ODD) == MISALIGNED and _norm(beta=ODD) == MISALIGNED
+    assert _norm_bwd(gy=None) == NULL and _norm_bwd(ws=None) == NULL
+    for k in ("gy", "res", "gx", "gg", "gb", "ws"):
+        assert _norm_bwd(**{k: ODD}) == MISALIGNED, k
+    assert _norm_bwd(nbytes=0) == WORKSPACE
+    n = ctypes.c_size_t()
+    assert tdn.lib().tdn_layer_norm_workspace_size(10, 2, 32, None) == NULL
+    assert tdn.lib().tdn_layer_norm_workspace_size(10, 7, 32, ctypes.byref(n)) == SHAPE
+    assert tdn.lib().tdn_layer_norm_workspace_size(10, 2, 32, ctypes.byref(n)) == 0 and n.value > 0
+    assert _norm_bwd(nbytes=n.value - 256) == WORKSPACE
+
+
+def _ffn(fwd, nbytes=1 << 40, **kw):
+    p = dict(n_nodes=10, L=2, C=32, n_hidden=64, dtype=0, act=0)
+    a = dict(x=FAKE, up=FAKE, gate=FAKE, b=FAKE, down=FAKE, res=FAKE, y=FAKE, ws=FAKE)
+    p.update({k: v for k, v in kw.items() if k in p})
+    a.update({k: v for k, v in kw.items() if k in a})
+    q = tdn.FfnProblem(*p.values())
+    if fwd:
+        return tdn.lib().tdn_gated_ffn_forward(ctypes.byref(q), a["x"], a["up"], a["gate"], a["b"], a["down"],
+                                               a["res"], a["y"], a["ws"], nbytes, None)
+    # grad_y in the residual's place, grad_x in y's
+    return tdn.lib().tdn_gated_ffn_backward(ctypes.byref(q), a["x"], a["up"], a["gate"], a["b"], a["down"], a["res"],
+                                            a["y"], FAKE, FAKE, FAKE, FAKE, a["ws"], nbytes, None)
+
+
+@pytest.mark.parametrize("fwd", [True, False])
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_nodes=-1), SHAPE), (dict(L=7), SHAPE), (dict(L=-1), SHAPE), (dict(C=24), SHAPE), (dict(C=0), SHAPE),
+    (dict(C=288), SHAPE), (dict(n_hidden=0), SHAPE), (dict(n_hidden=24), SHAPE), (dict(n_hidden=4112), SHAPE),
+    (dict(act=3), SHAPE), (dict(act=-1), SHAPE), (dict(dtype=2), DTYPE), (dict(n_nodes=(1 << 31) // 9), SHAPE)]
+    + [({k: None}, NULL) for k in ("x", "up", "gate", "down", "ws")]
+    + [({k: ODD}, MISALIGNED) for k in ("x", "up", "gate", "b", "down", "res", "y", "ws")])
+def test_gated_ffn_refusals(fwd, kw, status):
+    assert _ffn(fwd, **kw) == status
+
+
+def test_gated_ffn_workspace():
+    p = tdn.make_ffn_problem(10, 2, 32, 64)
+    f, b = tdn.gated_ffn_workspace_size(p)
+    assert 0 < f < b
+    assert _ffn(True, nbytes=f - 1) == WORKSPACE and _ffn(False, nbytes=b - 1) == WORKSPACE
+    assert _ffn(True, y=None) == NULL and _ffn(False, res=None) == NULL
+    assert tdn.lib().tdn_gated_ffn_forward(None, *[FAKE] * 8, 1 << 40, None) == NULL
+    assert tdn.lib().tdn_gated_ffn_workspace_size(ctypes.byref(p), None, None) == 0
+    with pytest.raises(ValueError):
+        tdn.make_ffn_problem(10, 2, 32, 64, activation="relu")
+
+
+def test_binding_refuses_wrong_tensors():
+    x, g = torch.zeros(4, 9, 32), torch.ones(3, 32)
+    w, wd = torch.zeros(32, 64), torch.zeros(64, 32)
+    for bad, e in [(x.double(), TypeError), (x[0], ValueError), (x[:, :8], ValueError),
+                   (x.transpose(0, 2), ValueError)]:
+        with pytest.raises(e):
+            tdn.layer_norm(bad, g)
+        with pytest.raises(e):
+            tdn.gated_ffn(bad, w, w, wd)
+    for bad, e in [(g.bfloat16(), TypeError), (g[:2], ValueError), (g.repeat(1, 2)[:, ::2], ValueError)]:
+        with pytest.raises(e):
+            tdn.layer_norm(x, bad)
+        with pytest.raises(e):
+            tdn.layer_norm_backward(x, bad, x)
+    for bad, e in [(x.bfloat16(), TypeError), (x[:3], ValueError)]:
+        with pytest.raises(e):
+            tdn.layer_norm_backward(x, g, bad)
+        with pytest.raises(e):
+            tdn.layer_norm_backward(x, g, x, grad_res=bad)
+        with pytest.raises(e):
+            tdn.gated_ffn(x, w, w, wd, residual=bad)
+        with pytest.raises(e):
+            tdn.gated_ffn_backward(x, w, w, wd, bad)
+    for args in [(w.bfloat16(), w, wd), (w, w[:, :32], wd), (w, w, w), (w[0], w, wd)]:
+        with pytest.raises((TypeError, ValueError)):
+            tdn.gated_ffn(x, *args)
+    with pytest.raises(ValueError):
+        tdn.gated_ffn(x, w, w, wd, out=x)
+    # tensors of the host are refused, not read
+    with pytest.raises(ValueError):
+        tdn.layer_norm(x, g)
+    with pytest.raises(ValueError):
+        tdn.gated_ffn(x, w, w, wd)

@@ -1,0 +1,176 @@
+"""GPU parity of the gated feed-forward block and its backward against the
+oracle (oracle/block.py, float64).
+
+Tolerances.  float32: the products run on two-part splits (2^-22 of each
+operand) with float32 sums over at most 4096 terms; the parity bound of the
+layer, 1e-5 of a node's largest value (of the tensor's for the weights'
+gradients), covers their chain.  bfloat16: each output has one rounding of an
+intermediate (2^-8 of its value, carried through the absolute values of the
+product that takes it) and its own (2^-8): `_bf16_bounds`."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_01131_amd as tdn
+from oracle import block
+from tests._gpu_helpers import TOL_F32, check_elementwise, check_rows
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = 2.0 ** -8  # half a step of bfloat16
+
+
+def _inputs(seed, N, L, C, F, dtype, bias=True):
+    gen = torch.Generator().manual_seed(seed)
+    d = (L + 1) ** 2
+    r = lambda *s: torch.randn(s, generator=gen)  # noqa: E731
+    t = lambda v: v.to(DT[dtype]).cuda()  # noqa: E731
+    return dict(x=t(r(N, d, C)), w_up=t(r(C, F) / C ** 0.5), w_gate=t(r(C, F) / C ** 0.5),
+                w_down=t(r(F, C) / F ** 0.5), b_gate=(0.3 * r(F)).cuda() if bias else None,
+                residual=t(r(N, d, C)), grad_y=t(r(N, d, C)))
+
+
+def _np(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def _bf16_bounds(i, act):
+    """Elementwise bounds of (y, grad_x, grad_w_up, grad_w_gate, grad_w_down)
+    beyond the rounding of the value itself, from one rounding of h, of
+    (grad_y w_down^T) act(q) and of dq."""
+    x, wu, wg, wd, gy = (_np(i[k]) for k in ("x", "w_up", "w_gate", "w_down", "grad_y"))
+    C, F = wu.shape
+    q = x[:, 0] @ wg + (0.0 if i["b_gate"] is None else _np(i["b_gate"]))
+    s, ds = block.activation(q, act)
+    u, dh = x @ wu, gy @ wd.T
+    h, du, dq = np.abs(u * s[:, None]), np.abs(dh * s[:, None]), np.abs((u * dh).sum(axis=1) * ds)
+    gx = du @ np.abs(wu.T)
+    gx[:, 0] += dq @ np.abs(wg.T)
+    flat = lambda v: np.abs(v).reshape(-1, v.shape[-1])  # noqa: E731
+    return [HALF * b for b in (h @ np.abs(wd), gx, flat(x).T @ du.reshape(-1, F), 0 * np.abs(wg),
+                               h.reshape(-1, F).T @ flat(gy))]
+
+
+def _check(gpu, ref, dtype, bound, what, rows):
+    assert gpu.dtype == DT[dtype]
+    g = _np(gpu)
+    if dtype == "f32":
+        check_rows(g, ref, TOL_F32, what) if rows else check_elementwise(g, ref, TOL_F32, what)
+        return
+    assert np.all(np.isfinite(g))
+    top = np.abs(ref).max(axis=(1, 2), keepdims=True) if rows else np.abs(ref).max()
+    err = np.abs(g - ref)
+    assert np.all(err <= bound + HALF * (np.abs(ref) + bound) + TOL_F32 * top), (what, (err / (bound + 1e-30)).max())
+
+
+def _run_and_check(i, act, dtype):
+    args = [i[k] for k in ("x", "w_up", "w_gate", "w_down")]
+    ref = [_np(a) for a in args]
+    bounds = _bf16_bounds(i, act) if dtype == "bf16" else [None] * 5
+    y0 = tdn.gated_ffn(*args, b_gate=i["b_gate"], activation=act)
+    _check(y0, block.gated_ffn(*ref, _np(i["b_gate"]), act=act), dtype, bounds[0], "y", True)
+    y = tdn.gated_ffn(*args, b_gate=i["b_gate"], residual=i["residual"], activation=act)
+    _check(y, block.gated_ffn(*ref, _np(i["b_gate"]), _np(i["residual"]), act), dtype, bounds[0], "y + residual", True)
+    grads = tdn.gated_ffn_backward(*args, i["grad_y"], b_gate=i["b_gate"], activation=act)
+    refs = block.gated_ffn_backward(*ref, _np(i["grad_y"]), _np(i["b_gate"]), act)
+    names = ("grad_x", "grad_w_up", "grad_w_gate", "grad_w_down")
+    for k, n in enumerate(names):
+        _check(grads[k], refs[k], dtype, bounds[1 + k], n, n == "grad_x")
+    if i["b_gate"] is None:
+        assert grads[4] is None
+    else:
+        check_elementwise(_np(grads[4]), refs[4], TOL_F32, "grad_b_gate")
+    return y, grads
+
+
+CASES = [
+    # N, L, C, F, act, bias
+    (1, 0, 16, 16, "silu", True), (1, 0, 256, 1024, "silu", True), (1, 6, 128, 48, "gelu", False),
+    (2, 1, 48, 80, "sigmoid", True), (40, 2, 16, 64, "silu", True), (33, 0, 256, 272, "gelu", True),
+    (129, 0, 64, 32, "silu", False), (37, 3, 80, 240, "gelu", False), (70, 4, 128, 160, "silu", True),
+    (23, 4, 256, 96, "sigmoid", True), (11, 5, 176, 112, "silu", True), (9, 6, 224, 64, "silu", False),
+    (600, 1, 96, 144, "silu", True), (300, 4, 160, 64, "gelu", True),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,L,C,F,act,bias", CASES)
+def test_forward_and_backward_match_the_oracle(N, L, C, F, act, bias, dtype):
+    _run_and_check(_inputs(N + 10 * L + C, N, L, C, F, dtype, bias), act, dtype)
+
+
+def test_rows_of_very_different_sizes():
+    """Rows scaled over 24 orders of magnitude: each keeps its own accuracy
+    (every row of fp32 products has its own power of two)."""
+    i = _inputs(5, 64, 2, 64, 96, "f32")
+    scale = torch.logspace(-12, 0, 64, device="cuda")[:, None, None]
+    i["x"] *= scale.flip(0)
+    i["grad_y"] *= scale
+    i["x"][7] = 0
+    i["grad_y"][9] = 0
+    i["x"][11, 0] = 0
+    i["w_up"][:, 32:64] *= 1e-9
+    i["w_down"][64:] *= 1e6
+    i["residual"] = torch.zeros_like(i["x"])
+    y, grads = _run_and_check(i, "silu", "f32")
+    assert torch.all(y[7] == 0) and torch.all(grads[0][9] == 0)
+
+
+def test_only_some_gradients():
+    i = _inputs(6, 50, 2, 64, 64, "f32")
+    args = [i[k] for k in ("x", "w_up", "w_gate", "w_down")] + [i["grad_y"]]
+    full = tdn.gated_ffn_backward(*args, b_gate=i["b_gate"])
+    x_only = tdn.gated_ffn_backward(*args, b_gate=i["b_gate"], need_weights=False)
+    w_only = tdn.gated_ffn_backward(*args, b_gate=i["b_gate"], need_x=False)
+    assert torch.equal(x_only[0], full[0]) and all(g is None for g in x_only[1:])
+    assert w_only[0] is None and all(torch.equal(p, q) for p, q in zip(w_only[1:], full[1:]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_nodes(dtype):
+    i = _inputs(7, 0, 1, 32, 48, dtype)
+    args = [i[k] for k in ("x", "w_up", "w_gate", "w_down")]
+    assert tdn.gated_ffn(*args, b_gate=i["b_gate"]).shape == (0, 4, 32)
+    grads = tdn.gated_ffn_backward(*args, i["grad_y"], b_gate=i["b_gate"])
+    assert grads[0].shape == (0, 4, 32) and all(torch.all(g == 0) for g in grads[1:])
+
+
+def test_a_bad_value_stays_in_its_node():
+    i = _inputs(8, 40, 1, 64, 64, "f32")
+    args = lambda: [i[k] for k in ("x", "w_up", "w_gate", "w_down")]  # noqa: E731
+    ref = tdn.gated_ffn(*args(), b_gate=i["b_gate"])
+    i["x"][5, 2, 3], i["x"][17, 0, 1] = float("nan"), float("inf")
+    y = tdn.gated_ffn(*args(), b_gate=i["b_gate"])
+    keep = torch.ones(40, 4, dtype=torch.bool, device="cuda")
+    keep[5, 2] = keep[17] = False
+    assert torch.equal(y[keep], ref[keep]) and torch.isnan(y[5, 2]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_repeat_calls_streams_in_place_and_graph_replays(dtype):
+    i = _inputs(9, 300, 3, 128, 192, dtype)
+    args = [i[k] for k in ("x", "w_up", "w_gate", "w_down")]
+
+    def step(**kw):
+        return [tdn.gated_ffn(*args, b_gate=i["b_gate"], residual=i["residual"], **kw),
+                *tdn.gated_ffn_backward(*args, i["grad_y"], b_gate=i["b_gate"], **kw)]
+
+    ref = step()
+    assert all(torch.equal(p, q) for p, q in zip(step(), ref))
+    r = i["residual"].clone()
+    assert torch.equal(tdn.gated_ffn(*args, b_gate=i["b_gate"], residual=r, out=r), ref[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    again = step(stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(p, q) for p, q in zip(again, ref))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(3):
+        if k == 2:
+            i["x"].copy_(i["x"].flip(0))
+            ref = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, ref))
