@@ -203,6 +203,31 @@ tdn_status tdn_attention_forward(const tdn_problem* p, int32_t n_heads, int32_t 
                                  const float* att_w2, float* out, float* alpha, float* z_save, int32_t* perm,
                                  int32_t* offsets, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* Its backward for the scalar <grad_out, out>: the weights alpha are
+ * recomputed (with the forward's kernels), the softmax's and the logits' MLP's
+ * gradients included.  Arguments as tdn_attention_forward; perm and offsets
+ * are its outputs, z_save its saved weighted sum or NULL (then it is
+ * recomputed).  Each gradient pointer may be NULL to skip it:
+ *   grad_x        [N, d, C]             through messages and logits
+ *   grad_W        [C, C]
+ *   grad_edge_vec [E, 3]                in the caller's original edge order
+ *   grad_radial_w [n_radial, R]
+ *   grad_att_w1   [2C + n_radial, n_hidden]
+ *   grad_att_w2   [n_hidden, n_heads]
+ * LeakyReLU's slope at 0 is 0.2.  A node without incoming edges takes no part.
+ * The CP factors are constants.  Every pointer 16-byte aligned
+ * (TDN_ERR_MISALIGNED); deterministic.  Workspace:
+ * tdn_attention_backward_workspace_size. */
+tdn_status tdn_attention_backward_workspace_size(const tdn_problem* p, int32_t n_heads, int32_t n_hidden,
+                                                 size_t* bytes);
+tdn_status tdn_attention_backward(const tdn_problem* p, int32_t n_heads, int32_t n_hidden, const float* x,
+                                  const float* edge_vec, const int32_t* edge_index, const float* A, const float* B,
+                                  const float* D, const float* W, const float* radial_w, const float* att_w1,
+                                  const float* att_w2, const int32_t* perm, const int32_t* offsets,
+                                  const float* z_save, const float* grad_out, float* grad_x, float* grad_W,
+                                  float* grad_edge_vec, float* grad_radial_w, float* grad_att_w1, float* grad_att_w2,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Measurement ablations of the forward's hot-path choices: the same layer
  * and arguments as tdn_cp_tp_forward (Sec. 3.1 eq. approximate, Sec. 3.2),
  * with one choice of the edge pass replaced (the paper attributes its speed
@@ -480,7 +505,7 @@ tdn_status tdn_spherical_harmonics(int32_t L, int32_t E, const float* edge_vec, 
  * "dense_edge_fwd", "dense_edge_unshared",
  * "path_gemm", "radius_graph", "edge_factors" (the launch before the layout where an edge pass
  * goes through per-edge matrices), "feature_layout",
- * "layer_norm", "layer_norm_bwd", "gated_ffn", "gated_ffn_bwd",
+ * "layer_norm", "layer_norm_bwd", "gated_ffn", "gated_ffn_bwd", "attention_bwd_dg", "attention_bwd_mlp",
  * "channel_layout", "cp_edge_bwd_src", "cp_bwd_dst", "radial_grad", "node_gemm", "gram",
  * "sort");
  * reset = 1 clears that kernel's record. */

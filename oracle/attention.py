@@ -25,6 +25,7 @@ from __future__ import annotations
 import numpy as np
 
 from .layer import edge_terms, radial_basis, stable_sort_by_key
+from .sh import spherical_harmonics, spherical_harmonics_jacobian
 
 LEAKY_SLOPE = 0.2
 
@@ -78,3 +79,62 @@ def forward(x, edge_index, edge_vec, A, B, D, W, radial_w, W1, w2, r_cut, L, per
         zsum[dst[e]] += alpha[e][head][None, :] * z
     out = zsum @ W
     return (out, alpha, zsum) if return_z else (out, alpha)
+
+
+def backward(x, edge_index, edge_vec, A, B, D, W, radial_w, W1, w2, r_cut, L, grad_out, absolute=False):
+    """(grad_x, grad_W, grad_edge_vec, grad_radial_w, grad_W1, grad_w2) of the
+    scalar <grad_out, out>, per edge: the product rule on alpha_e z_e, the
+    softmax's Jacobian and the MLP's.  LeakyReLU's slope at 0 is the negative
+    side's.  absolute: the same chain with every factor and term replaced by
+    its absolute value (alpha as it is), which bounds what cancels in each
+    gradient (an error scale, not a value)."""
+    f = (lambda v: np.abs(np.asarray(v, np.float64))) if absolute else (lambda v: np.asarray(v, np.float64))
+    alpha_all = segment_softmax(logits(x, edge_index, edge_vec, W1, w2, r_cut, np.asarray(radial_w).shape[0]),
+                                edge_index[1], np.asarray(x).shape[0])
+    vec_in, G = np.asarray(edge_vec, np.float64), f(grad_out)
+    x, A, B, D, W, Wr, W1, w2 = (f(v) for v in (x, A, B, D, W, radial_w, W1, w2))
+    N, d, C = x.shape
+    H, nr = w2.shape[1], Wr.shape[0]
+    src, dst = np.asarray(edge_index, np.int64)
+    E = src.shape[0]
+    Ch = C // H
+    gx, gW, gvec, gWr = np.zeros_like(x), np.zeros_like(W), np.zeros((E, 3)), np.zeros_like(Wr)
+    dalpha, dg_all = np.zeros((E, H)), np.zeros((E, A.shape[1]))
+    Gz = G @ W.T
+    dist = np.linalg.norm(vec_in, axis=1)
+    phi_all, dphi_all = (f(v) for v in radial_basis(dist, r_cut, nr))
+    Y_all = f(spherical_harmonics(L, vec_in))
+    for c0 in range(0, E, 256):
+        e = slice(c0, min(E, c0 + 256))
+        s, t = src[e], dst[e]
+        v, rho = Y_all[e] @ B, phi_all[e] @ Wr
+        g = v * rho
+        u = np.matmul(A.T[None], x[s])                          # [e, R, C]
+        Gh = np.matmul(D.T[None], Gz[t])                        # [e, R, C], per unit weight
+        a = np.repeat(alpha_all[e], Ch, axis=1)                 # [e, C]
+        z = np.matmul(D[None], g[:, :, None] * u)               # [e, d, C]
+        gW += np.einsum("edc,edf->cf", z * a[:, None], G[t])
+        dalpha[e] = (z * Gz[t]).sum(axis=1).reshape(-1, H, Ch).sum(axis=2)
+        dg_all[e] = (Gh * u * a[:, None]).sum(axis=2)
+        np.add.at(gx, s, np.matmul(A[None], g[:, :, None] * Gh * a[:, None]))
+    sign = 1.0 if absolute else -1.0
+    dot = np.zeros((N, H))
+    np.add.at(dot, dst, alpha_all * dalpha)
+    da = alpha_all * (dalpha + sign * dot[dst])
+    q = np.concatenate([x[dst, 0], x[src, 0], phi_all], axis=1)
+    hid = q @ W1
+    slope = np.ones_like(hid) if absolute else np.where(hid > 0, 1.0, LEAKY_SLOPE)
+    act = slope * hid
+    dhid = slope * (da @ w2.T)
+    gw2, gW1 = act.T @ da, q.T @ dhid
+    dq = dhid @ W1.T
+    np.add.at(gx, (dst, 0), dq[:, :C])
+    np.add.at(gx, (src, 0), dq[:, C:2 * C])
+    v, rho = Y_all @ B, phi_all @ Wr
+    drho = dg_all * v
+    gWr = phi_all.T @ drho
+    dphi = drho @ Wr.T + dq[:, 2 * C:]
+    J = f(spherical_harmonics_jacobian(L, vec_in))
+    gvec = np.einsum("ek,ekx->ex", (dg_all * rho) @ B.T, J)
+    gvec += ((dphi * dphi_all).sum(axis=1) / dist)[:, None] * f(vec_in)
+    return gx, gW, gvec, gWr, gW1, gw2

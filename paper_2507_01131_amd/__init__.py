@@ -21,8 +21,8 @@ from dataclasses import dataclass
 import torch
 
 __all__ = ["forward", "backward", "sort_by_key", "spherical_harmonics", "workspace_size", "Problem",
-           "TdnError", "layer_norm", "layer_norm_backward", "gated_ffn", "gated_ffn_backward", "lib", "timer_enable",
-           "timer_read", "LIB_PATH", "status_string"]
+           "TdnError", "attention_forward", "attention_backward", "layer_norm", "layer_norm_backward", "gated_ffn",
+           "gated_ffn_backward", "lib", "timer_enable", "timer_read", "LIB_PATH", "status_string"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtdn.so")
 
@@ -87,6 +87,8 @@ def lib() -> ctypes.CDLL:
         L.tdn_ablation_workspace_size.argtypes = [PP, ctypes.c_int32, ctypes.POINTER(_SZ)]
         L.tdn_attention_workspace_size.argtypes = [PP, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(_SZ)]
         L.tdn_attention_forward.argtypes = [PP, ctypes.c_int32, ctypes.c_int32] + [_P] * 16 + [_SZ, _P]
+        L.tdn_attention_backward_workspace_size.argtypes = [PP, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(_SZ)]
+        L.tdn_attention_backward.argtypes = [PP, ctypes.c_int32, ctypes.c_int32] + [_P] * 21 + [_SZ, _P]
         L.tdn_ablation_forward.argtypes = [PP, ctypes.c_int32] + [_P] * 13 + [_SZ, _P]
         L.tdn_dense_tp_forward_unshared.argtypes = [PP] + [_P] * 6 + [ctypes.c_int32] + [_P] * 6 + [_SZ, _P]
         GP = ctypes.POINTER(GraphProblem)
@@ -116,7 +118,8 @@ def lib() -> ctypes.CDLL:
                   "tdn_cp_tp3_forward", "tdn_ps_linear_workspace_size", "tdn_ps_linear",
                   "tdn_dense_tp_unshared_workspace_size", "tdn_dense_tp_forward_unshared",
                   "tdn_ablation_workspace_size", "tdn_ablation_forward", "tdn_attention_workspace_size",
-                  "tdn_attention_forward", "tdn_layer_norm_forward", "tdn_layer_norm_workspace_size",
+                  "tdn_attention_forward", "tdn_attention_backward_workspace_size", "tdn_attention_backward",
+                  "tdn_layer_norm_forward", "tdn_layer_norm_workspace_size",
                   "tdn_layer_norm_backward", "tdn_gated_ffn_workspace_size", "tdn_gated_ffn_forward",
                   "tdn_gated_ffn_backward"):
             getattr(L, f).restype = ctypes.c_int
@@ -644,7 +647,58 @@ def attention_forward(x, edge_vec, edge_index, A, B, D, W, radial_w, att_w1, att
                                      _ptr(workspace), workspace.numel(), _stream(stream))
     _check(st, "tdn_attention_forward")
     return ForwardResult(out, z, perm, offsets, p, dict(x=x, edge_vec=edge_vec, edge_index=edge_index, A=A, B=B,
-                                                        D=D, W=W, radial_w=radial_w)), alpha
+                                                        D=D, W=W, radial_w=radial_w, att_w1=att_w1,
+                                                        att_w2=att_w2)), alpha
+
+
+def attention_backward_workspace_size(p: Problem, n_heads: int, n_hidden: int) -> int:
+    """Workspace bytes of tdn_attention_backward."""
+    nb = _SZ(0)
+    _check(lib().tdn_attention_backward_workspace_size(ctypes.byref(p), int(n_heads), int(n_hidden),
+                                                       ctypes.byref(nb)), "tdn_attention_backward_workspace_size")
+    return nb.value
+
+
+def attention_backward(res: ForwardResult, grad_out, *, need_x=True, need_W=True, need_vec=True, need_radial=True,
+                       need_att=True, workspace=None, stream=None):
+    """Runs tdn_attention_backward on attention_forward's result (its z, if it
+    was given one, is the saved weighted sum).  Returns (grad_x, grad_W,
+    grad_edge_vec, grad_radial_w, grad_att_w1, grad_att_w2), float32 or None
+    where not needed."""
+    i = res.inputs
+    if "att_w1" not in i or "att_w2" not in i:
+        raise ValueError("not the result of attention_forward")
+    x = i["x"]
+    dev = x.device
+    N, d, C = x.shape
+    E = i["edge_vec"].shape[0]
+    F, H = i["att_w2"].shape
+    p = res.problem
+    if (p.n_nodes, (p.L + 1) ** 2, p.C, p.n_edges) != (N, d, C, E):
+        raise ValueError("the result's problem is not that of its inputs")
+    R, nr = p.R, p.n_radial
+    for n, sh in [("x", (N, d, C)), ("edge_vec", (E, 3)), ("A", (d, R)), ("B", (d, R)), ("D", (d, R)), ("W", (C, C)),
+                  ("radial_w", (nr, R)), ("att_w1", (2 * C + nr, F)), ("att_w2", (F, H))]:
+        _need(i[n], n, torch.float32, sh, dev)
+    _need(i["edge_index"], "edge_index", torch.int32, (2, E), dev)
+    _need(res.perm, "perm", torch.int32, (E,), dev)
+    _need(res.offsets, "offsets", torch.int32, (N + 1,), dev)
+    if res.z is not None:
+        _need(res.z, "z", torch.float32, (N, d, C), dev)
+    _need(grad_out, "grad_out", torch.float32, (N, d, C), dev)
+    with _launching(dev, stream) as s:
+        workspace = _workspace(workspace, attention_backward_workspace_size(p, H, F), dev)
+        make = lambda need, like: torch.empty_like(like) if need else None  # noqa: E731
+        gx, gW, gv = make(need_x, x), make(need_W, i["W"]), make(need_vec, i["edge_vec"])
+        gr, g1, g2 = make(need_radial, i["radial_w"]), make(need_att, i["att_w1"]), make(need_att, i["att_w2"])
+        _check(lib().tdn_attention_backward(ctypes.byref(p), int(H), int(F), _ptr(x), _ptr(i["edge_vec"]),
+                                            _ptr(i["edge_index"]), _ptr(i["A"]), _ptr(i["B"]), _ptr(i["D"]),
+                                            _ptr(i["W"]), _ptr(i["radial_w"]), _ptr(i["att_w1"]), _ptr(i["att_w2"]),
+                                            _ptr(res.perm), _ptr(res.offsets), _ptr(res.z), _ptr(grad_out), _ptr(gx),
+                                            _ptr(gW), _ptr(gv), _ptr(gr), _ptr(g1), _ptr(g2), _ptr(workspace),
+                                            workspace.numel() * workspace.element_size(), _stream(s)),
+               "tdn_attention_backward")
+    return gx, gW, gv, gr, g1, g2
 
 
 def dense_unshared_workspace_size(p: Problem) -> int:

@@ -39,6 +39,13 @@ tdn_status hip_fail(hipError_t e) {
 
 int dim_of(int L) { return (L + 1) * (L + 1); }
 
+// whether every pointer is 16-byte aligned (NULL is)
+bool aligned16(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return false;
+  return true;
+}
+
 // Ranks: the edge kernels take at most kChunkR; larger ranks (up to
 // kMaxRank, e.g. the exact rank d^2 construction of Thm. 2) run as chunks of
 // consecutive 32-rank tiles, balanced, whose per-node results are summed in
@@ -647,6 +654,251 @@ tdn_status tdn_attention_forward(const tdn_problem* p, int32_t n_heads, int32_t 
   return TDN_OK;
 }
 
+namespace {
+struct AttBwdLayout {
+  size_t gz, z, xt, xp, gp, part, parts, perm_src, off_src, sort, wp, Pt, Ps, al, al_eid, al_src, g, dg, dal, dhid,
+      dPt, dPs, part_da, sum_da, part_w1, wrad, gv, ops, flags, total;
+};
+// x (or Gz) in the packed layout, then its row scales
+size_t packed_bytes(const tdn_problem& p) {
+  return al(size_t(p.n_nodes) * (p.C / 32) * 256 * tdn::pk_rows(dim_of(p.L)));
+}
+AttBwdLayout att_bwd_layout(const tdn_problem& p, int H, int F) {
+  AttBwdLayout b{};
+  const size_t N = p.n_nodes, E = p.n_edges, ndc = N * dim_of(p.L) * p.C * 4, RT = (p.R + 31) / 32;
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o += al(bytes);
+    return at;
+  };
+  b.gz = take(ndc);
+  b.z = take(ndc);
+  b.xt = take(xt_bytes(p));
+  b.xp = take(packed_bytes(p) + N * 4);
+  b.gp = take(packed_bytes(p) + N * 4);
+  b.part = take(partial_bytes(p));
+  b.parts = take(size_t(tdn::gram_parts(p.n_nodes * dim_of(p.L), p.C)) * p.C * p.C * 4);
+  b.perm_src = take(E * 4);
+  b.off_src = take((N + 1) * 4);
+  b.sort = take(tdn::sort_plan(p.n_nodes, p.n_edges).bytes);
+  b.wp = take(tdn::node_gemm_ws_bytes(p.C));
+  b.Pt = take(N * F * 4);
+  b.Ps = take(N * F * 4);
+  b.al = take(E * H * 4);
+  b.al_eid = take(E * H * 4);
+  b.al_src = take(E * H * 4);
+  b.g = take(E * p.R * 4);
+  b.dg = take(E * p.R * 4);
+  b.dal = take(RT * E * H * 4);
+  b.dhid = take(E * F * 4);
+  b.dPt = take(N * F * 4);
+  b.dPs = take(N * F * 4);
+  b.part_da = take(size_t(tdn::att_bwd_da_blocks(p.n_nodes)) * (p.n_radial + H) * F * 4);
+  b.sum_da = take(size_t(p.n_radial + H) * F * 4);
+  b.part_w1 = take(size_t(tdn::att_bwd_dw1_parts(p.n_nodes)) * 2 * p.C * F * 4);
+  b.wrad = take(size_t(2 * tdn::device_cus()) * p.n_radial * p.R * 4);
+  b.gv = take(E * 12);
+  b.ops = take(tdn::att_bwd_ops_bytes(dim_of(p.L), p.R));
+  b.flags = take(256);
+  b.total = o;
+  return b;
+}
+}  // namespace
+
+tdn_status tdn_attention_backward_workspace_size(const tdn_problem* p, int32_t n_heads, int32_t n_hidden,
+                                                 size_t* bytes) {
+  const tdn_status st = check_attention(p, n_heads, n_hidden);
+  if (st != TDN_OK) return st;
+  if (!bytes) return TDN_ERR_NULL_POINTER;
+  *bytes = att_bwd_layout(*p, n_heads, n_hidden).total;
+  return TDN_OK;
+}
+
+tdn_status tdn_attention_backward(const tdn_problem* p, int32_t n_heads, int32_t n_hidden, const float* x,
+                                  const float* edge_vec, const int32_t* edge_index, const float* A, const float* B,
+                                  const float* D, const float* W, const float* radial_w, const float* att_w1,
+                                  const float* att_w2, const int32_t* perm, const int32_t* offsets,
+                                  const float* z_save, const float* grad_out, float* grad_x, float* grad_W,
+                                  float* grad_edge_vec, float* grad_radial_w, float* grad_att_w1, float* grad_att_w2,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  tdn_status st = check_attention(p, n_heads, n_hidden);
+  if (st != TDN_OK) return st;
+  const int N = p->n_nodes, E = p->n_edges, d = dim_of(p->L), C = p->C, F = n_hidden, H = n_heads, R = p->R;
+  if (!A || !B || !D || !W || !radial_w || !att_w1 || !att_w2 || !offsets || !workspace) return TDN_ERR_NULL_POINTER;
+  if (N > 0 && (!x || !grad_out)) return TDN_ERR_NULL_POINTER;
+  if (E > 0 && (!edge_vec || !edge_index || !perm)) return TDN_ERR_NULL_POINTER;
+  if (!aligned16({x, edge_vec, edge_index, A, B, D, W, radial_w, att_w1, att_w2, perm, offsets, z_save, grad_out,
+                  grad_x, grad_W, grad_edge_vec, grad_radial_w, grad_att_w1, grad_att_w2, workspace}))
+    return TDN_ERR_MISALIGNED;
+  const AttBwdLayout lay = att_bwd_layout(*p, H, F);
+  if (workspace_bytes < lay.total) return TDN_ERR_WORKSPACE_TOO_SMALL;
+  st = check_device();
+  if (st != TDN_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  if (p->validate) {
+    st = run_validation(*p, edge_index, edge_vec, ws, lay.flags, 0, stream);
+    if (st != TDN_OK) return st;
+  }
+  if (E == 0) {  // no message: the output is zero whatever the inputs
+    const std::pair<float*, size_t> all[] = {
+        {grad_x, size_t(N) * d * C},           {grad_W, size_t(C) * C},
+        {grad_radial_w, size_t(p->n_radial) * R}, {grad_att_w1, size_t(2 * C + p->n_radial) * F},
+        {grad_att_w2, size_t(F) * H}};
+    for (const auto& g : all)
+      if (g.first && g.second) TDN_HIP(tdn::launch_zero(g.first, g.second * 4, stream));
+    return TDN_OK;
+  }
+  auto f = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  auto i32 = [&](size_t off) { return reinterpret_cast<int32_t*>(ws + off); };
+  const int32_t *src = edge_index, *dst = edge_index + E;
+  const bool mat = use_mat(*p);
+  float* Gz = f(lay.gz);
+  {
+    Timed t("node_gemm", stream);
+    TDN_HIP(tdn::launch_node_gemm(N * d, C, grad_out, W, false, 1, Gz, ws + lay.wp, stream));
+  }
+  {
+    Timed t("attention_weights", stream);
+    TDN_HIP(tdn::launch_att_node(N, d, C, F, x, att_w1, f(lay.Pt), f(lay.Ps), stream));
+    TDN_HIP(tdn::launch_att_alpha(N, C, F, H, p->n_radial, p->r_cut / float(p->n_radial - 1), offsets, perm, src,
+                                  edge_vec, f(lay.Pt), f(lay.Ps), att_w1, att_w2, f(lay.al), f(lay.al_eid), stream));
+  }
+  if (grad_W) {
+    const float* Z = z_save;
+    if (!Z) {
+      TDN_HIP(edge_features(*p, x, true, mat, A, D, B, radial_w, ws + lay.part, ws + lay.xt, stream));
+      Timed t("cp_edge_fwd_att", stream);
+      tdn::EdgeArgs a = edge_args(*p, offsets, perm, src, dst, edge_vec, A, D, B, radial_w, ws + lay.xt, f(lay.z),
+                                  f(lay.part));
+      a.alpha = f(lay.al);
+      a.n_heads = H;
+      TDN_HIP(mat ? tdn::launch_cp_edge_mat(a, stream) : tdn::launch_cp_edge_att(a, stream));
+      Z = f(lay.z);
+    }
+    Timed t("gram", stream);
+    TDN_HIP(tdn::launch_gram(N * d, C, Z, grad_out, false, f(lay.parts), grad_W, stream));
+  }
+  if (!grad_x && !grad_edge_vec && !grad_radial_w && !grad_att_w1 && !grad_att_w2) return TDN_OK;
+
+  tdn::AttBwdArgs a{};
+  a.N = N;
+  a.E = E;
+  a.L = p->L;
+  a.d = d;
+  a.C = C;
+  a.R = R;
+  a.H = H;
+  a.F = F;
+  a.n_radial = p->n_radial;
+  a.sigma = p->r_cut / float(p->n_radial - 1);
+  a.offsets = offsets;
+  a.perm = perm;
+  a.off_src = i32(lay.off_src);
+  a.perm_src = i32(lay.perm_src);
+  a.src = src;
+  a.dst = dst;
+  a.edge_vec = edge_vec;
+  a.A = A;
+  a.B = B;
+  a.D = D;
+  a.radial_w = radial_w;
+  a.x = x;
+  a.W1 = att_w1;
+  a.w2 = att_w2;
+  a.xp = ws + lay.xp;
+  a.gp = ws + lay.gp;
+  float* x_scale = f(lay.xp + packed_bytes(*p));
+  float* g_scale = f(lay.gp + packed_bytes(*p));
+  a.x_scale = x_scale;
+  a.g_scale = g_scale;
+  a.ops = ws + lay.ops;
+  a.Pt = f(lay.Pt);
+  a.Ps = f(lay.Ps);
+  a.alpha = f(lay.al);
+  a.alpha_eid = f(lay.al_eid);
+  a.alpha_src = f(lay.al_src);
+  a.g = f(lay.g);
+  a.dg = f(lay.dg);
+  a.dal = f(lay.dal);
+  a.dhid = f(lay.dhid);
+  a.dPt = f(lay.dPt);
+  a.dPs = f(lay.dPs);
+  a.part_da = f(lay.part_da);
+  a.sum_da = f(lay.sum_da);
+  a.part_w1 = f(lay.part_w1);
+  a.grad_vec = grad_edge_vec;
+  a.grad_w1 = grad_att_w1;
+  a.grad_w2 = grad_att_w2;
+  {
+    Timed t("feature_layout", stream);
+    TDN_HIP(tdn::launch_feature_layout_packed(N, d, C, x, ws + lay.xp, x_scale, stream));
+    TDN_HIP(tdn::launch_feature_layout_packed(N, d, C, Gz, ws + lay.gp, g_scale, stream));
+  }
+  {
+    Timed t("attention_bwd_dg", stream);
+    TDN_HIP(tdn::launch_att_bwd_dg(a, stream));
+  }
+  if (grad_edge_vec || grad_radial_w) {
+    tdn::BwdDstArgs b{};
+    b.n_seg = N;
+    b.E = E;
+    b.L = p->L;
+    b.d = d;
+    b.C = C;
+    b.R = R;
+    b.n_radial = p->n_radial;
+    b.sigma = a.sigma;
+    b.offsets = offsets;
+    b.perm = perm;
+    b.src = src;
+    b.dst = dst;
+    b.edge_vec = edge_vec;
+    b.A = A;
+    b.Bf = B;
+    b.D = D;
+    b.radial_w = radial_w;
+    b.grad_vec = grad_edge_vec ? grad_edge_vec : f(lay.gv);
+    b.x_scale = x_scale;
+    b.dg = a.dg;
+    b.dg_given = true;
+    const tdn::EdgePlan dp = tdn::bwd_dst_plan(p->L, R, C, p->n_radial, false, E, true);
+    if (dp.n_range < 1) return hip_fail(hipErrorInvalidValue);
+    b.n_range = dp.n_range;
+    b.pieces_per_block = dp.per_block;
+    b.wrad_part = grad_radial_w ? f(lay.wrad) : nullptr;
+    {
+      Timed t("cp_bwd_dst", stream);
+      TDN_HIP(tdn::launch_bwd_dst(b, false, stream));
+    }
+    if (grad_radial_w) {
+      Timed t("radial_grad", stream);
+      TDN_HIP(tdn::launch_sum_parts(dp.n_range / dp.per_block, p->n_radial * R, b.wrad_part, grad_radial_w, stream));
+    }
+  }
+  {
+    Timed t("sort", stream);
+    TDN_HIP(tdn::launch_sort(tdn::sort_plan(N, E), src, 1, i32(lay.perm_src), i32(lay.off_src), ws + lay.sort, stream));
+  }
+  {
+    Timed t("attention_bwd_mlp", stream);
+    TDN_HIP(tdn::launch_att_bwd_mlp(a, stream));
+  }
+  if (!grad_x) return TDN_OK;
+  TDN_HIP(edge_features(*p, Gz, true, mat, D, A, B, radial_w, ws + lay.part, ws + lay.xt, stream));
+  {
+    Timed t("cp_edge_bwd_src", stream);
+    tdn::EdgeArgs e = edge_args(*p, a.off_src, a.perm_src, dst, src, edge_vec, D, A, B, radial_w, ws + lay.xt, grad_x,
+                                f(lay.part));
+    e.alpha = a.alpha_src;
+    e.n_heads = H;
+    TDN_HIP(mat ? tdn::launch_cp_edge_mat(e, stream) : tdn::launch_cp_edge_att(e, stream));
+  }
+  Timed t("attention_bwd_mlp", stream);
+  TDN_HIP(tdn::launch_att_bwd_x0(a, grad_x, stream));
+  return TDN_OK;
+}
+
 tdn_status tdn_cp_tp3_forward(const tdn_problem* p, const void* x, const float* edge_vec, const int32_t* edge_index,
                               const float* A, const float* A2, const float* B, const float* D, const void* W,
                               const float* radial_w, float* out, float* z_save, int32_t* perm, int32_t* offsets,
@@ -721,12 +973,6 @@ tdn_status tdn_ps_linear(int32_t n_nodes, int32_t L, int32_t C, const float* x, 
 }
 
 namespace {
-// whether every pointer is 16-byte aligned (NULL is)
-bool aligned16(std::initializer_list<const void*> ptrs) {
-  for (const void* p : ptrs)
-    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return false;
-  return true;
-}
 tdn_status check_norm(int32_t n_nodes, int32_t L, int32_t C) {
   if (n_nodes < 0 || L < 0 || L > 6 || C < 16 || C > 256 || C % 16 != 0) return TDN_ERR_BAD_SHAPE;
   if (int64_t(n_nodes) * dim_of(L) >= (int64_t(1) << 31) - 4096) return TDN_ERR_BAD_SHAPE;

@@ -35,12 +35,12 @@ bool bwd_dst_split(int L, int C, bool bf16) {
   return (L + 1) * (L + 1) <= 32 && bwd2_detail::dst2_split(C, bf16);
 }
 
-EdgePlan bwd_dst_plan(int L, int R, int C, int n_radial, bool bf16, int E) {
+EdgePlan bwd_dst_plan(int L, int R, int C, int n_radial, bool bf16, int E, bool dg_given) {
   using namespace bwd2_detail;
   const int d = (L + 1) * (L + 1);
   const int RT = (R + kTile - 1) / kTile;
   if (E <= 0 || d > 32 || RT > 8) return EdgePlan{0, 0};
-  const bool split = bwd_dst_split(L, C, bf16);
+  const bool split = dg_given || bwd_dst_split(L, C, bf16);
   const int chunk = dst2_chunk(RT, bf16, d, n_radial, C, split);
   const int lds = dst2_smem(RT, bf16 ? 1 : 2, d, n_radial, C, chunk, split).floats * 4;
   if (lds > 160 * 1024) return EdgePlan{0, 0};
@@ -60,7 +60,7 @@ int bwd_dst_cpad(int C, bool bf16) { return bwd2_detail::dst2_cpad(C, bf16 ? 1 :
 hipError_t launch_bwd_dst(const BwdDstArgs& a, bool x_bf16, hipStream_t s) {
   if (a.n_seg == 0 || a.E == 0) return hipSuccess;
   if (a.n_range > 0) {
-    if (a.d > 32 || a.n_range > a.E || !a.xc || !a.dst || (!x_bf16 && !a.x_scale)) return hipErrorInvalidValue;
+    if (a.d > 32 || a.n_range > a.E || (!a.xc && !a.dg_given) || !a.dst || (!x_bf16 && !a.x_scale)) return hipErrorInvalidValue;
     switch (a.L) {
 #define TDN_DST2_CASE(LV)                                                  \
   case LV:                                                                 \

@@ -912,8 +912,9 @@ hipError_t launch_l_rt(const BwdDstArgs& a, int n_range, hipStream_t s) {
   if (a.pieces_per_block < 1 || n_range % a.pieces_per_block) return hipErrorInvalidValue;
   constexpr int d = (L + 1) * (L + 1);
   // a Gz layout given: the split form, dg first
-  const bool split = a.gzc != nullptr;
-  if (split) {
+  const bool split = a.gzc != nullptr || a.dg_given;
+  if (a.dg_given && !a.dg) return hipErrorInvalidValue;
+  if (split && !a.dg_given) {
     if (!a.dg || (!BF && !a.gz_scale) || !dst2_split(a.C, BF)) return hipErrorInvalidValue;
     const hipError_t e = launch_dg<L, RT, BF>(a, s);
     if (e != hipSuccess) return e;

@@ -162,6 +162,39 @@ hipError_t launch_att_alpha(int N, int C, int F, int H, int n_radial, float sigm
                             const int32_t* perm, const int32_t* src, const float* edge_vec, const float* Pt,
                             const float* Ps, const float* W1, const float* w2, float* alpha_sorted,
                             float* alpha_eid, hipStream_t s);
+// The block's backward (attention_bwd.hip; 1 <= L <= 4, R <= 256, fp32).
+// launch_att_bwd_dg: dg [E, R] by sorted position and the rank tiles' shares
+// dal [ceil(R / 32), E, H] of dalpha, from x and Gz in the packed layout.
+// launch_att_bwd_mlp: the softmax and the logits' MLP; adds to grad_vec (if
+// not nullptr), and writes dhid, dPt, dPs, alpha_src, grad_w1 and grad_w2 (the
+// last two may be nullptr).  launch_att_bwd_x0: adds what the logits owe to
+// the degree-0 rows of grad_x.
+struct AttBwdArgs {
+  int N, E, L, d, C, R, H, F, n_radial;
+  float sigma;
+  const int32_t *offsets, *perm;          // by destination
+  const int32_t *off_src, *perm_src;      // by source
+  const int32_t *src, *dst;               // [E] by edge id
+  const float *edge_vec, *A, *B, *D, *radial_w, *x, *W1, *w2;
+  const void *xp, *gp;                    // x, Gz: launch_feature_layout_packed's words
+  const float *x_scale, *g_scale;         // and row scales
+  void* ops;                              // att_bwd_ops_bytes
+  const float *Pt, *Ps;                   // launch_att_node
+  const float *alpha, *alpha_eid;         // [E, H] by sorted position, by edge id
+  float* alpha_src;                       // [E, H] in the order of perm_src
+  float *g, *dg, *dal;                    // [E, R], [E, R], [ceil(R / 32), E, H]
+  float *dhid, *dPt, *dPs;                // [E, F] by edge id, [N, F], [N, F]
+  float *part_da, *sum_da;                // [att_bwd_da_blocks(N)][n_radial + H][F], [n_radial + H][F]
+  float* part_w1;                         // [att_bwd_dw1_parts(N)][2 C][F]
+  float *grad_vec, *grad_w1, *grad_w2;
+};
+size_t att_bwd_ops_bytes(int d, int R);
+int att_bwd_da_blocks(int N);
+int att_bwd_dw1_parts(int N);
+hipError_t launch_att_bwd_dg(const AttBwdArgs& a, hipStream_t s);
+hipError_t launch_att_bwd_mlp(const AttBwdArgs& a, hipStream_t s);
+hipError_t launch_att_bwd_place(const AttBwdArgs& a, hipStream_t s);
+hipError_t launch_att_bwd_x0(const AttBwdArgs& a, float* grad_x, hipStream_t s);
 // Measurement ablations of the edge pass (fp32 features, 2 <= L <= 4, one
 // rank chunk), each with one hot-path choice replaced:
 //   kAblFactorsGlobal: the packed factor blocks read in the edge loop from a
@@ -297,12 +330,15 @@ struct BwdDstArgs {
   const float* gz_scale;    // fp32 problems: row_scale of that layout
   float* dg;                // split form: [E, R] dL/dg by sorted edge position (written, then read);
                             // direct form: by edge id, may be drho
+  bool dg_given;            // range kernel: a.dg holds dL/dg by sorted position already (the split form's
+                            // second kernel alone; xc, x and Gz are not read, x_scale is)
 };
 // Edge ranges of the destination-side kernel on the current device
 // (n_range = 0 when the problem takes the per-segment kernels: d > 32 or no
 // LDS fit): per_block ranges per workgroup, workgroup b taking ranges
 // b, b + n_range / per_block, ...
-EdgePlan bwd_dst_plan(int L, int R, int C, int n_radial, bool bf16, int E);
+// dg_given: the plan of a launch with that field set.
+EdgePlan bwd_dst_plan(int L, int R, int C, int n_radial, bool bf16, int E, bool dg_given = false);
 // whether the range kernel takes the split form for this channel count (the
 // contraction over channels in a kernel of its own, Gz[t] held in registers)
 bool bwd_dst_split(int L, int C, bool bf16);

@@ -118,3 +118,33 @@ def test_binding_refuses_wrong_tensors():
         tdn.layer_norm(x, g)
     with pytest.raises(ValueError):
         tdn.gated_ffn(x, w, w, wd)
+
+
+def _att(nbytes=1 << 40, heads=2, hidden=8, **kw):
+    p = dict(L=2, C=64, R=32, n_nodes=10, n_edges=40, r_cut=5.0, feat_dtype=0)
+    p.update({k: v for k, v in kw.items() if k in p})
+    names = ["x", "vec", "ei", "A", "B", "D", "W", "rw", "w1", "w2", "perm", "off", "z", "go", "gx", "gW", "gv", "gr",
+             "g1", "g2"]
+    a = {n: kw.get(n, FAKE) for n in names}
+    q = tdn.make_problem(**p)
+    return tdn.lib().tdn_attention_backward(ctypes.byref(q), heads, hidden, *a.values(), kw.get("ws", FAKE), nbytes,
+                                            None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(heads=0), SHAPE), (dict(heads=4), SHAPE), (dict(heads=9), SHAPE), (dict(hidden=0), SHAPE),
+    (dict(hidden=65), SHAPE), (dict(L=0), SHAPE), (dict(L=5), SHAPE), (dict(R=257), SHAPE), (dict(C=48), SHAPE),
+    (dict(feat_dtype=1), DTYPE), (dict(n_nodes=0), SHAPE)]
+    + [({k: None}, NULL) for k in ("x", "vec", "ei", "A", "B", "D", "W", "rw", "w1", "w2", "perm", "off", "go", "ws")]
+    + [({k: ODD}, MISALIGNED) for k in ("x", "vec", "ei", "perm", "off", "z", "go", "gx", "gW", "gv", "gr", "g1",
+                                        "g2", "ws")])
+def test_attention_backward_refusals(kw, status):
+    assert _att(**kw) == status
+
+
+def test_attention_backward_workspace():
+    p = tdn.make_problem(2, 64, 32, 10, 40, 5.0)
+    n = tdn.attention_backward_workspace_size(p, 2, 8)
+    assert n > 0 and _att(nbytes=n - 1) == WORKSPACE
+    with pytest.raises(tdn.TdnError):
+        tdn.attention_backward_workspace_size(p, 4, 8)

@@ -1,0 +1,196 @@
+"""GPU parity of the attention block's backward against the oracle
+(oracle/attention.py, float64): every gradient on small problems over the
+degrees, head counts and odd sizes it supports, nodes without edges, one edge
+alone, a star, saved and recomputed sums, chosen gradients, repeat calls, other
+streams and graph replays.
+
+Tolerances: the layer's parity bounds (1e-5 per tensor, per node, and per edge
+with its conditioning; tests/_gpu_helpers.py).  What reaches the logits' MLP
+passes the softmax's difference dalpha - sum(alpha dalpha), which cancels where
+one weight dominates; its gradients are held to 1e-5 of the larger of the
+tensor's largest value and the same chain on absolute values over its median
+conditioning.  LeakyReLU's slope jumps at 0, so the problems have no hidden
+value within 1e-5 of it (checked before the comparison)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_01131_amd as tdn
+import workloads
+from oracle import attention, layer
+from tests._gpu_helpers import TOL_F32, check_elementwise, check_rows, check_scaled, random_factors, rel_err
+
+pytestmark = pytest.mark.gpu
+
+
+def _t(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _problem(seed, L, C, R, H, F, N, E, srt, n_radial=8):
+    w = workloads.random_graph(900 + seed, n_nodes=N, n_edges=E, L=L, C=C, R=R, sort=srt)
+    rng = np.random.default_rng(seed)
+    if n_radial != 8:
+        w["n_radial"] = n_radial
+        w["radial_w"] = (rng.standard_normal((n_radial, R)) / np.sqrt(n_radial)).astype(np.float32)
+    w["W1"] = (2 * rng.standard_normal((2 * C + n_radial, F)) / np.sqrt(2 * C + n_radial)).astype(np.float32)
+    w["w2"] = (2 * rng.standard_normal((F, H)) / np.sqrt(F)).astype(np.float32)
+    w["factors"] = random_factors(L, R, seed)
+    return w
+
+
+def _clear_of_the_kink(w, margin=1e-5):
+    """Moves the source features of edges with a hidden value near 0."""
+    for _ in range(20):
+        x, (src, dst) = w["x"].astype(np.float64), w["edge_index"].astype(np.int64)
+        phi, _ = layer.radial_basis(np.linalg.norm(w["edge_vec"].astype(np.float64), axis=1), w["r_cut"],
+                                    w["n_radial"])
+        hid = np.concatenate([x[dst, 0], x[src, 0], phi], axis=1) @ w["W1"].astype(np.float64)
+        bad = np.unique(src[np.abs(hid).min(axis=1) < margin])
+        if not bad.size:
+            return
+        w["x"][bad, 0] += np.float32(0.01)
+    raise AssertionError("hidden values near 0")
+
+
+def _run(w, z=True, **kw):
+    A, B, D = w["factors"]
+    res, _ = tdn.attention_forward(
+        _t(w["x"]), _t(w["edge_vec"]), _t(w["edge_index"]), _t(A), _t(B), _t(D), _t(w["W"]), _t(w["radial_w"]),
+        _t(w["W1"]), _t(w["w2"]), L=w["L"], r_cut=w["r_cut"], edges_sorted=w["presorted"],
+        z=torch.empty(w["x"].shape, device="cuda") if z else None)
+    return res, tdn.attention_backward(res, _t(w["grad_out"]), **kw)
+
+
+def _oracle(w, absolute=False):
+    A, B, D = w["factors"]
+    return attention.backward(w["x"], w["edge_index"], w["edge_vec"], A, B, D, w["W"], w["radial_w"], w["W1"], w["w2"],
+                              w["r_cut"], w["L"], w["grad_out"], absolute)
+
+
+def _check(grads, w):
+    g = [v.cpu().numpy() for v in grads]
+    ref, scale = _oracle(w), _oracle(w, absolute=True)
+    check_rows(g[0], ref[0], TOL_F32, "grad_x")
+    check_elementwise(g[1], ref[1], TOL_F32, "grad_W")
+    assert rel_err(g[2], ref[2]) < TOL_F32
+    check_scaled(g[2], ref[2], scale[2], TOL_F32, "grad_edge_vec")
+    check_elementwise(g[3], ref[3], TOL_F32, "grad_radial_w")
+    for k, what in ((4, "grad_att_w1"), (5, "grad_att_w2")):
+        pos = np.abs(ref[k]) > 0
+        c = np.median(scale[k][pos] / np.abs(ref[k][pos])) if pos.any() else 1.0
+        bound = np.maximum(np.abs(ref[k]).max(), scale[k] / c)
+        err = np.abs(g[k] - ref[k])
+        assert np.all(np.isfinite(g[k])) and np.all(err <= TOL_F32 * bound), (what, (err / bound).max())
+
+
+CASES = [
+    # seed, L, C, R, H, F, N, E, sorted, n_radial
+    (1, 1, 32, 32, 1, 8, 30, 300, False, 8), (2, 2, 64, 32, 2, 16, 40, 600, True, 8),
+    (3, 3, 64, 64, 2, 32, 50, 800, False, 8), (4, 4, 128, 128, 4, 32, 60, 1200, False, 8),
+    (5, 4, 128, 100, 1, 64, 40, 700, True, 16), (6, 2, 128, 48, 4, 7, 35, 500, False, 2),
+    (7, 4, 256, 200, 8, 33, 20, 400, False, 5), (8, 3, 192, 256, 2, 1, 25, 300, True, 8),
+    (9, 1, 96, 1, 3, 12, 15, 90, False, 8), (10, 4, 160, 33, 5, 64, 300, 700, False, 3),
+    (11, 4, 64, 96, 2, 24, 1, 70, False, 8),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"L{c[1]}C{c[2]}R{c[3]}H{c[4]}F{c[5]}")
+def test_every_gradient_matches_the_oracle(case):
+    w = _problem(*case)
+    _clear_of_the_kink(w)
+    _check(_run(w)[1], w)
+
+
+@pytest.mark.parametrize("L,C,R,H", [(2, 64, 32, 2), (4, 128, 128, 4)])
+def test_a_star_single_edges_and_empty_nodes(L, C, R, H):
+    w = _problem(20, L, C, R, H, 16, 90, 760, False)
+    w["edge_index"][1, :700] = 3            # 700 edges into one node
+    w["edge_index"][1, 700:] = 20 + np.arange(60)  # one edge each
+    w["edge_index"][0, :] %= 60             # nodes from 60 on: no edge out; many without one in
+    _clear_of_the_kink(w)
+    res, grads = _run(w)
+    _check(grads, w)
+    touched = np.zeros(90, bool)
+    touched[w["edge_index"].ravel()] = True
+    assert np.all(grads[0].cpu().numpy()[~touched] == 0)
+
+
+def test_one_edge_has_no_gradient_of_the_logits():
+    w = _problem(21, 3, 64, 64, 2, 16, 5, 1, False)
+    _, grads = _run(w)
+    ref = _oracle(w)
+    for g, r in zip(grads[:4], ref):
+        assert rel_err(g.cpu().numpy(), r) < TOL_F32
+    # alpha = 1: dalpha - sum(alpha dalpha) is an exact zero
+    assert torch.all(grads[4] == 0) and torch.all(grads[5] == 0)
+
+
+def test_no_edges():
+    w = _problem(22, 2, 64, 32, 2, 16, 12, 0, False)
+    _, grads = _run(w)
+    assert all(torch.all(g == 0) for g in grads) and grads[2].shape == (0, 3)
+
+
+def test_recomputed_sum_and_chosen_gradients():
+    w = _problem(23, 4, 128, 128, 4, 32, 60, 1200, False)
+    res, full = _run(w)
+    _, again = _run(w, z=False)
+    assert rel_err(again[1].cpu().numpy(), full[1].cpu().numpy()) < 1e-6
+    for k in (0, 2, 3, 4, 5):
+        assert torch.equal(again[k], full[k])
+    g = _t(w["grad_out"])
+    need = ("need_x", "need_W", "need_vec", "need_radial")
+    for k, n in enumerate(need):
+        only = tdn.attention_backward(res, g, **{m: m == n for m in need}, need_att=False)
+        assert torch.equal(only[k], full[k]) and all(v is None for j, v in enumerate(only) if j != k)
+    only = tdn.attention_backward(res, g, **{m: False for m in need})
+    assert torch.equal(only[4], full[4]) and torch.equal(only[5], full[5])
+
+
+@pytest.mark.parametrize("N,E", [(120, 3000), (700, 50001)])
+def test_repeat_calls_streams_and_graph_replays(N, E):
+    # (the larger one goes through per-edge matrices)
+    w = _problem(24, 4, 128, 128, 4, 32, N, E, False)
+    res, ref = _run(w)
+    g = _t(w["grad_out"])
+    assert all(torch.equal(a, b) for a, b in zip(tdn.attention_backward(res, g), ref))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = tdn.attention_backward(res, g, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(other, ref))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = tdn.attention_backward(res, g)
+    for k in range(3):
+        if k == 2:
+            g.copy_(g.flip(0))
+            ref = tdn.attention_backward(res, g)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, ref))
+
+
+def test_equal_weights_give_the_plain_layers_gradients():
+    """Two GPU paths: w2 = 0 gives alpha = 1 / in-degree, so the messages'
+    gradients are the plain backward's of grad_out / in-degree."""
+    w = _problem(25, 3, 64, 64, 2, 16, 50, 900, False)
+    w["w2"][:] = 0
+    _, grads = _run(w)
+    deg = np.maximum(np.bincount(w["edge_index"][1], minlength=50), 1).astype(np.float32)
+    A, B, D = w["factors"]
+    plain = tdn.forward(_t(w["x"]), _t(w["edge_vec"]), _t(w["edge_index"]), _t(A), _t(B), _t(D), _t(w["W"]),
+                        _t(w["radial_w"]), L=3, r_cut=w["r_cut"])
+    ref = tdn.backward(plain, _t(w["grad_out"] / deg[:, None, None]), need_radial=True)
+    for a, b in zip(grads[:4], ref):
+        assert rel_err(a.cpu().numpy(), b.cpu().numpy()) < TOL_F32
+
+
+def test_refuses_another_result():
+    w = _problem(26, 2, 64, 32, 2, 16, 12, 30, False)
+    A, B, D = w["factors"]
+    plain = tdn.forward(_t(w["x"]), _t(w["edge_vec"]), _t(w["edge_index"]), _t(A), _t(B), _t(D), _t(w["W"]),
+                        _t(w["radial_w"]), L=2, r_cut=w["r_cut"])
+    with pytest.raises(ValueError):
+        tdn.attention_backward(plain, _t(w["grad_out"]))
