@@ -12,7 +12,6 @@ the library is not built -- there is no fallback implementation.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -159,6 +158,9 @@ def workspace_size(p: Problem) -> tuple[int, int]:
 
 
 def _need(t, name, dtype, shape, device):
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device \
+            and t.is_contiguous():
+        return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor")
     if t.dtype != dtype:
@@ -353,19 +355,39 @@ def ps_linear(x, W, *, workspace=None, out=None, stream=None):
     return out
 
 
-@contextlib.contextmanager
-def _launching(dev, stream):
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+class _launching:
     """The tensors' device and the stream made current (the given stream, or
     the device's current one), so that scratch memory allocated inside belongs
-    to the stream that uses it."""
-    if dev.type != "cuda":
-        raise ValueError(f"tensors on {dev}: the library runs on a GPU")
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    elif stream.device != dev:
-        raise ValueError(f"stream on {stream.device}, tensors on {dev}")
-    with torch.cuda.stream(stream):     # (sets the device too)
-        yield stream
+    to the stream that uses it; gives the stream's handle."""
+    __slots__ = ("stream", "scope")
+
+    def __init__(self, dev, stream):
+        if dev.type != "cuda":
+            raise ValueError(f"tensors on {dev}: the library runs on a GPU")
+        self.scope = None
+        if stream is None:
+            stream = torch.cuda.current_stream(dev)
+            if dev.index != torch.cuda.current_device():
+                self.scope = torch.cuda.stream(stream)     # (sets the device too)
+        elif stream.device != dev:
+            raise ValueError(f"stream on {stream.device}, tensors on {dev}")
+        else:
+            self.scope = torch.cuda.stream(stream)
+        self.stream = stream
+
+    def __enter__(self):
+        if self.scope is not None:
+            self.scope.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+        return False
 
 
 def _feature_dtype(x, name="x"):
@@ -406,8 +428,8 @@ def layer_norm(x, gamma, beta=None, *, eps: float = 1e-5, out=None, stream=None)
     with _launching(dev, stream) as s:
         if out is None:
             out = torch.empty_like(x)
-        _check(lib().tdn_layer_norm_forward(N, L, C, dt, float(eps), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(out),
-                                            _stream(s)), "tdn_layer_norm_forward")
+        _check(lib().tdn_layer_norm_forward(N, L, C, dt, float(eps), _addr(x), _addr(gamma), _addr(beta), _addr(out),
+                                            s), "tdn_layer_norm_forward")
     return out
 
 
@@ -431,9 +453,9 @@ def layer_norm_backward(x, gamma, grad_y, *, eps: float = 1e-5, grad_res=None, n
         gx = torch.empty_like(x) if need_x else None
         gg = torch.empty((L + 1, C), dtype=torch.float32, device=dev) if need_weights else None
         gb = torch.empty((C,), dtype=torch.float32, device=dev) if need_weights else None
-        _check(lib().tdn_layer_norm_backward(N, L, C, dt, float(eps), _ptr(x), _ptr(gamma), _ptr(grad_y),
-                                             _ptr(grad_res), _ptr(gx), _ptr(gg), _ptr(gb), _ptr(workspace),
-                                             workspace.numel() * workspace.element_size(), _stream(s)),
+        _check(lib().tdn_layer_norm_backward(N, L, C, dt, float(eps), _addr(x), _addr(gamma), _addr(grad_y),
+                                             _addr(grad_res), _addr(gx), _addr(gg), _addr(gb), _addr(workspace),
+                                             workspace.numel() * workspace.element_size(), s),
                "tdn_layer_norm_backward")
     return gx, gg, gb
 
@@ -487,9 +509,9 @@ def gated_ffn(x, w_up, w_gate, w_down, *, b_gate=None, residual=None, activation
         workspace = _workspace(workspace, gated_ffn_workspace_size(p)[0], dev)
         if out is None:
             out = torch.empty_like(x)
-        _check(lib().tdn_gated_ffn_forward(ctypes.byref(p), _ptr(x), _ptr(w_up), _ptr(w_gate), _ptr(b_gate),
-                                           _ptr(w_down), _ptr(residual), _ptr(out), _ptr(workspace),
-                                           workspace.numel() * workspace.element_size(), _stream(s)),
+        _check(lib().tdn_gated_ffn_forward(ctypes.byref(p), _addr(x), _addr(w_up), _addr(w_gate), _addr(b_gate),
+                                           _addr(w_down), _addr(residual), _addr(out), _addr(workspace),
+                                           workspace.numel() * workspace.element_size(), s),
                "tdn_gated_ffn_forward")
     return out
 
@@ -507,10 +529,10 @@ def gated_ffn_backward(x, w_up, w_gate, w_down, grad_y, *, b_gate=None, activati
         gx = torch.empty_like(x) if need_x else None
         gu, gg, gd = (torch.empty_like(w) if need_weights else None for w in (w_up, w_gate, w_down))
         gb = torch.empty_like(b_gate) if need_weights and b_gate is not None else None
-        _check(lib().tdn_gated_ffn_backward(ctypes.byref(p), _ptr(x), _ptr(w_up), _ptr(w_gate), _ptr(b_gate),
-                                            _ptr(w_down), _ptr(grad_y), _ptr(gx), _ptr(gu), _ptr(gg), _ptr(gb),
-                                            _ptr(gd), _ptr(workspace),
-                                            workspace.numel() * workspace.element_size(), _stream(s)),
+        _check(lib().tdn_gated_ffn_backward(ctypes.byref(p), _addr(x), _addr(w_up), _addr(w_gate), _addr(b_gate),
+                                            _addr(w_down), _addr(grad_y), _addr(gx), _addr(gu), _addr(gg), _addr(gb),
+                                            _addr(gd), _addr(workspace),
+                                            workspace.numel() * workspace.element_size(), s),
                "tdn_gated_ffn_backward")
     return gx, gu, gg, gd, gb
 
@@ -691,12 +713,12 @@ def attention_backward(res: ForwardResult, grad_out, *, need_x=True, need_W=True
         make = lambda need, like: torch.empty_like(like) if need else None  # noqa: E731
         gx, gW, gv = make(need_x, x), make(need_W, i["W"]), make(need_vec, i["edge_vec"])
         gr, g1, g2 = make(need_radial, i["radial_w"]), make(need_att, i["att_w1"]), make(need_att, i["att_w2"])
-        _check(lib().tdn_attention_backward(ctypes.byref(p), int(H), int(F), _ptr(x), _ptr(i["edge_vec"]),
-                                            _ptr(i["edge_index"]), _ptr(i["A"]), _ptr(i["B"]), _ptr(i["D"]),
-                                            _ptr(i["W"]), _ptr(i["radial_w"]), _ptr(i["att_w1"]), _ptr(i["att_w2"]),
-                                            _ptr(res.perm), _ptr(res.offsets), _ptr(res.z), _ptr(grad_out), _ptr(gx),
-                                            _ptr(gW), _ptr(gv), _ptr(gr), _ptr(g1), _ptr(g2), _ptr(workspace),
-                                            workspace.numel() * workspace.element_size(), _stream(s)),
+        _check(lib().tdn_attention_backward(ctypes.byref(p), int(H), int(F), _addr(x), _addr(i["edge_vec"]),
+                                            _addr(i["edge_index"]), _addr(i["A"]), _addr(i["B"]), _addr(i["D"]),
+                                            _addr(i["W"]), _addr(i["radial_w"]), _addr(i["att_w1"]), _addr(i["att_w2"]),
+                                            _addr(res.perm), _addr(res.offsets), _addr(res.z), _addr(grad_out), _addr(gx),
+                                            _addr(gW), _addr(gv), _addr(gr), _addr(g1), _addr(g2), _addr(workspace),
+                                            workspace.numel() * workspace.element_size(), s),
                "tdn_attention_backward")
     return gx, gW, gv, gr, g1, g2
 

@@ -522,24 +522,37 @@ struct WgradArgs {
   float* partial;                 // [gridDim.y][2][C][32 FT]: W_down's (as [c][f]), then W_up's
 };
 
-// hidden tiles per pair of waves: what 512 registers hold
-__host__ __device__ constexpr int wgrad_tiles(int CT, bool BF) { return BF || CT <= 4 ? 2 : 1; }
+// Waves of a workgroup: two a SIMD where a wave's packed weights and sums leave
+// room in 256 registers.  A pair of waves has one tile of 32 hidden units.
+__host__ __device__ constexpr int wgrad_waves(int CT, bool BF) { return BF || CT <= 6 ? 8 : 4; }
 // LDS words: x and grad_y in both operand orders, then u and p of the pairs
 __host__ __device__ constexpr int wgrad_words(int CT, bool BF) {
-  return 4 * 2 * CT * (BF ? 1 : 2) * kBlk + 2 * 2 * wgrad_tiles(CT, BF) * 4 * kBlk;
+  return 4 * 2 * CT * (BF ? 1 : 2) * kBlk + wgrad_waves(CT, BF) * 4 * kBlk;
 }
 
+// four channels of a row as they lie in memory
+template <bool BF>
+struct Raw4 {
+  f32x4 v;
+};
+template <>
+struct Raw4<true> {
+  uint2 v;
+};
+
 template <int CT, bool BF>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_ffn_wgrad(WgradArgs a) {
-  constexpr int P = BF ? 1 : 2, NF = wgrad_tiles(CT, BF);
+__global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
+    __attribute__((amdgpu_waves_per_eu(wgrad_waves(CT, BF) / 4, wgrad_waves(CT, BF) / 4))) void k_ffn_wgrad(
+        WgradArgs a) {
+  constexpr int P = BF ? 1 : 2, NT = wgrad_waves(CT, BF) * kWave;
   constexpr int kOp = 2 * CT * P * kBlk;
-  constexpr int kItems = (64 * CT + 255) / 256;  // 4 x 4 blocks of a 32-row tile per thread and tensor
+  constexpr int kItems = (64 * CT + NT - 1) / NT;  // 4 x 4 blocks of a 32-row tile per thread and tensor
   extern __shared__ u32x4 smem[];
   __shared__ uint32_t s_max[2][32];
   __shared__ float s_rowf[32];
   __shared__ int s_eb;
-  u32x4* sU = smem + 4 * kOp;                                      // [pair][NF][4][64]
-  float* sP = reinterpret_cast<float*>(sU + 2 * NF * 4 * kBlk);     // [pair][NF][32 rows][32]
+  u32x4* sU = smem + 4 * kOp;                                                    // [pair][4][64]
+  float* sP = reinterpret_cast<float*>(sU + wgrad_waves(CT, BF) / 2 * 4 * kBlk);  // [pair][32 rows][32]
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int role = wave & 1, g = wave >> 1;  // role 0: u and grad W_down; 1: dh and grad W_up
@@ -547,77 +560,82 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   const int n0 = int(int64_t(blockIdx.y) * a.N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * a.N / gridDim.y);
   const int r0 = n0 * d, r1 = n1 * d;
   // a pair without a tile of its own repeats the last one and stores nothing
-  int ft[NF];
-  bool own[NF];
-  u32x4 w[NF][2 * CT][P];
-  int ew[NF], e_other[NF];
-#pragma unroll
-  for (int j = 0; j < NF; ++j) {
-    const int t = (blockIdx.x * 2 + g) * NF + j;
-    own[j] = t < FT;
-    ft[j] = min(t, FT - 1);
-    const u32x4* src = (role == 0 ? a.up_u : a.up_d) + size_t(ft[j]) * kOp + lane;
+  const int tile = blockIdx.x * (wgrad_waves(CT, BF) / 2) + g, ft = min(tile, FT - 1);
+  const bool own = tile < FT;
+  u32x4 w[2 * CT][P];
+  {
+    const u32x4* src = (role == 0 ? a.up_u : a.up_d) + size_t(ft) * kOp + lane;
 #pragma unroll
     for (int st = 0; st < 2 * CT; ++st)
 #pragma unroll
-      for (int p = 0; p < P; ++p) w[j][st][p] = src[(st * P + p) * kBlk];
-    ew[j] = BF ? 0 : (role == 0 ? a.e_u : a.e_d)[ft[j]];
-    e_other[j] = BF ? 0 : (role == 0 ? a.e_d : a.e_u)[ft[j]];
+      for (int p = 0; p < P; ++p) w[st][p] = src[(st * P + p) * kBlk];
   }
+  const int e_own = BF ? 0 : (role == 0 ? a.e_u : a.e_d)[ft], e_both = BF ? 0 : a.e_u[ft] + a.e_d[ft];
   // LDS: x in row order, x in transposed order, then grad_y in both
   const u32x4* rows_op = smem + (role == 0 ? 0 : 2) * kOp + lane;  // x for u, grad_y for dh
   const u32x4* cols_op = smem + (role == 0 ? 3 : 1) * kOp + lane;  // grad_y for W_down, x for W_up
-  f32x16 acc[NF][CT];
-  int E[NF];
+  f32x16 acc[CT];
+  int E = kUnset;
 #pragma unroll
-  for (int j = 0; j < NF; ++j) {
-    E[j] = kUnset;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) acc[j][ct] = f32x16{};
-  }
-  // this lane's running sum over a node's rows (waves of role 0: one lane a
-  // hidden unit of the pair's tiles), and the row's place in its node
+  for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x16{};
+  // rows to nodes without a division: (row - first row of node nb) / d for
+  // values up to d + 31 <= 80, as a product with ceil(2^16 / d) (exact there)
+  const uint32_t inv_d = (65536u + d - 1) / d;
+  // this lane's running sum over a node's rows (waves of role 0, one lane a
+  // hidden unit), and the next row's place in its node
   float run = 0.f;
   int in_node = 0, node = n0;
-  const int sum_j = NF == 2 ? lane >> 5 : 0;
-  const bool sums = role == 0 && (NF == 2 || h == 0) && (blockIdx.x * 2 + g) * NF + sum_j < FT;
-  const int sum_f = 32 * min((int(blockIdx.x) * 2 + g) * NF + sum_j, FT - 1) + l32;
+  const bool sums = own && h == 0;
   auto add_rows = [&](int n) {  // the first n rows of sP
-    for (int r = 0; r < n; ++r) {
-      run += sP[((g * NF + sum_j) * 32 + r) * 32 + l32];
-      if (++in_node == d) {
-        if (sums) a.dq[size_t(node) * Fp + sum_f] = run * a.ds[size_t(node) * Fp + sum_f];
-        run = 0.f;
-        in_node = 0;
-        ++node;
+    const float* p = sP + g * 1024 + l32;
+    for (int q = 0; q < n; q += 8) {
+      float v[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) v[r] = p[(q + r) * 32];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        if (q + r >= n) break;
+        run += v[r];
+        if (++in_node == d) {
+          if (sums) a.dq[size_t(node) * Fp + 32 * ft + l32] = run * a.ds[size_t(node) * Fp + 32 * ft + l32];
+          run = 0.f;
+          in_node = 0;
+          ++node;
+        }
       }
     }
   };
-  f32x4 vx[kItems][4], vg[kItems][4];
+  Raw4<BF> vx[kItems][4], vg[kItems][4];
+  auto raw = [&](const void* p, size_t row, uint32_t i) {  // the row is uniform, i the lane's
+    if constexpr (BF)
+      return Raw4<BF>{*reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + row * C + i)};
+    else
+      return Raw4<BF>{*reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + row * C + i)};
+  };
   auto fetch = [&](int rb) {
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      const int i = tid + 256 * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
+      const int i = tid + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int row = rb + 4 * rg + r;
-        const bool on = i < 64 * CT && c < C && row < r1;
-        vx[k][r] = on ? load4<BF>(a.x, size_t(row) * C + c) : f32x4{};
-        vg[k][r] = on ? load4<BF>(a.gy, size_t(row) * C + c) : f32x4{};
+        const bool on = i < 64 * CT && c < C && rb + 4 * rg + r < r1;
+        const uint32_t at = 4 * rg * C + c;
+        vx[k][r] = on ? raw(a.x, size_t(rb + r), at) : Raw4<BF>{};
+        vg[k][r] = on ? raw(a.gy, size_t(rb + r), at) : Raw4<BF>{};
       }
     }
   };
   // a 4 x 4 block into both operand orders
-  auto put = [&](const f32x4 (&v)[4], int rg, int c, u32x4* op, const float* sc) {
+  auto put = [&](const Raw4<BF> (&v)[4], int rg, int c, u32x4* op, const float* sc) {
     uint32_t hl[P][4][2];  // [part][row][pair of channels]
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         if constexpr (BF)
-          hl[0][r][k] = pack_bf16x2_rne(v[r][2 * k], v[r][2 * k + 1]);
+          hl[0][r][k] = k == 0 ? v[r].v.x : v[r].v.y;
         else
-          split_f16x2_pair(v[r][2 * k] * sc[r], v[r][2 * k + 1] * sc[r], hl[0][r][k], hl[1][r][k]);
+          split_f16x2_pair(v[r].v[2 * k] * sc[r], v[r].v[2 * k + 1] * sc[r], hl[0][r][k], hl[1][r][k]);
       }
     const int st = c >> 4, hh = (c >> 3) & 1;
     const int ct = c >> 5, q = rg >> 2, ht = rg & 1, it = (rg >> 1) & 1;
@@ -639,20 +657,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   };
   if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
   fetch(r0);
-  int prev = 0;  // rows of the tile before, whose products wait in sP
+  int prev = 0;                  // rows of the tile before, whose products wait in sP
+  int nb = n0, mb = 0;           // the tile's first row: row mb of node nb
   for (int rb = r0; rb < r1; rb += 32) {
     __syncthreads();  // s_max is zero; the tile before is consumed
     if constexpr (!BF) {
 #pragma unroll
       for (int k = 0; k < kItems; ++k) {
-        const int i = tid + 256 * k, rg = i / (8 * CT);
+        const int i = tid + NT * k, rg = i / (8 * CT);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float mx = 0.f, mg = 0.f;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            mx = fmaxf(mx, fabsf(vx[k][r][c]));
-            mg = fmaxf(mg, fabsf(vg[k][r][c]));
+            mx = fmaxf(mx, fabsf(vx[k][r].v[c]));
+            mg = fmaxf(mg, fabsf(vg[k][r].v[c]));
           }
 #pragma unroll
           for (int o = 4; o > 0; o >>= 1) {
@@ -679,7 +698,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     }
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      const int i = tid + 256 * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
+      const int i = tid + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
       if (i < 64 * CT) {
         float sx[4], sg[4];
         if constexpr (!BF) {
@@ -698,57 +717,56 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     if constexpr (!BF)
       if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
     // u or dh of the tile: rows in registers, hidden units in lanes
-    f32x16 t[NF];
-#pragma unroll
-    for (int j = 0; j < NF; ++j) t[j] = f32x16{};
+    f32x16 t = f32x16{};
 #pragma unroll
     for (int st = 0; st < 2 * CT; ++st) {
       u32x4 op[P];
 #pragma unroll
       for (int p = 0; p < P; ++p) op[p] = rows_op[(st * P + p) * kBlk];
+      t = mm_parts<BF>(op, w[st], t);
+    }
+    // the gate of this lane's hidden unit for its rows' nodes
+    float s[16];
+    const float* sp = a.s + size_t(nb) * Fp + 32 * ft + l32;
 #pragma unroll
-      for (int j = 0; j < NF; ++j) t[j] = mm_parts<BF>(op, w[j][st], t[j]);
+    for (int v = 0; v < 16; ++v) {
+      const int o = min(acc_row(v, h), r1 - 1 - rb);
+      s[v] = sp[int((uint32_t(mb + o) * inv_d) >> 16) * Fp];
     }
     if (role == 0) {
 #pragma unroll
-      for (int j = 0; j < NF; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          sU[((g * NF + j) * 4 + k) * kBlk + lane] =
-              __builtin_bit_cast(u32x4, f32x4{t[j][4 * k], t[j][4 * k + 1], t[j][4 * k + 2], t[j][4 * k + 3]});
+      for (int k = 0; k < 4; ++k)
+        sU[(g * 4 + k) * kBlk + lane] =
+            __builtin_bit_cast(u32x4, f32x4{t[4 * k], t[4 * k + 1], t[4 * k + 2], t[4 * k + 3]});
       add_rows(prev);
     }
     prev = min(32, r1 - rb);
+    mb += 32;
+    const int step = int((uint32_t(mb) * inv_d) >> 16);
+    nb += step;
+    mb -= step * d;
     __syncthreads();
     const int eb = BF ? 0 : s_eb;
-    float rowf[16];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) rowf[v] = BF ? 1.f : s_rowf[acc_row(v, h)];
-    u32x4 o[NF][2][P];
-#pragma unroll
-    for (int j = 0; j < NF; ++j) {
+    for (int k = 0; k < 4; ++k) {
+      // rows 8 k + 4 h .. + 3
+      const f32x4 rf = BF ? f32x4{1.f, 1.f, 1.f, 1.f} : *reinterpret_cast<const f32x4*>(s_rowf + 8 * k + 4 * h);
       if (role == 1) {
+        const f32x4 u = __builtin_bit_cast(f32x4, sU[(g * 4 + k) * kBlk + lane]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const f32x4 u = __builtin_bit_cast(f32x4, sU[((g * NF + j) * 4 + k) * kBlk + lane]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = u[i] * rowf[4 * k + i] * t[j][4 * k + i];
-            sP[((g * NF + j) * 32 + acc_row(4 * k + i, h)) * 32 + l32] = BF ? p : ldexpf(p, eb + ew[j] + e_other[j]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          const float p = u[i] * rf[i] * t[4 * k + i];
+          sP[(g * 32 + 8 * k + 4 * h + i) * 32 + l32] = BF ? p : ldexpf(p, eb + e_both);
         }
       }
-      float v16[16];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int row = min(rb + acc_row(v, h), r1 - 1);
-        v16[v] = t[j][v] * rowf[v] * a.s[size_t(row / d) * Fp + 32 * ft[j] + l32];
-      }
-      to_operand<BF>(v16, eb, E[j], o[j], [&](float f) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) acc[j][ct] *= f;
-      });
+      for (int i = 0; i < 4; ++i) s[4 * k + i] *= t[4 * k + i] * rf[i];
     }
+    u32x4 o[2][P];
+    to_operand<BF>(s, eb, E, o, [&](float f) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) acc[ct] *= f;
+    });
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -756,73 +774,63 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         u32x4 op[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) op[p] = cols_op[((2 * ct + q) * P + p) * kBlk];
-#pragma unroll
-        for (int j = 0; j < NF; ++j) acc[j][ct] = mm_parts<BF>(op, o[j][q], acc[j][ct]);
+        acc[ct] = mm_parts<BF>(op, o[q], acc[ct]);
       }
   }
   __syncthreads();
   if (role == 0) add_rows(prev);
+  if (!own) return;
+  float* out = a.partial + (size_t(blockIdx.y) * 2 + role) * C * Fp + 32 * ft + l32;
 #pragma unroll
-  for (int j = 0; j < NF; ++j) {
-    if (!own[j]) continue;
-    float* out = a.partial + (size_t(blockIdx.y) * 2 + role) * C * Fp + 32 * ft[j] + l32;
+  for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int c = 32 * ct + acc_row(v, h);
-        if (c < C) out[size_t(c) * Fp] = BF ? acc[j][ct][v] : ldexpf(acc[j][ct][v], E[j] + ew[j]);
-      }
-  }
+    for (int v = 0; v < 16; ++v) {
+      const int c = 32 * ct + acc_row(v, h);
+      if (c < C) out[size_t(c) * Fp] = BF ? acc[ct][v] : ldexpf(acc[ct][v], E + e_own);
+    }
 }
 
-// The ranges' sums in range order: a workgroup takes a 32 x 32 tile of one of
-// W_down's (z = 0, transposed on the way), W_up's (1) or W_gate's (2)
-// gradient; with z = 2 the first channel tile also takes grad b.
+// The ranges' sums in a fixed order: a workgroup takes 32 hidden units and four
+// channels of one of W_down's (z = 0), W_up's (1) or W_gate's (2) gradient,
+// eight threads a column each a strided share of the ranges, added in order;
+// with z = 2 the first channels' workgroups also take grad b.
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ffn_wsum(int C, int F, int FT, int S, int Sg,
                                                   const float* __restrict__ partial,
                                                   const float* __restrict__ partial_g, void* __restrict__ gd,
                                                   void* __restrict__ gu, void* __restrict__ gg,
                                                   float* __restrict__ gb) {
-  __shared__ float tile[32][33];
-  const int Fp = 32 * FT, c0 = 32 * blockIdx.y, f0 = 32 * blockIdx.x, z = blockIdx.z;
-  const int col = threadIdx.x & 31, r8 = threadIdx.x >> 5;
+  __shared__ float red[8][5][32];
+  const int Fp = 32 * FT, c0 = 4 * blockIdx.y, z = blockIdx.z;
+  const int col = threadIdx.x & 31, k = threadIdx.x >> 5, f = 32 * blockIdx.x + col;
   void* out = z == 0 ? gd : (z == 1 ? gu : gg);
-  auto put = [&](size_t i, float v) {
-    if constexpr (BF)
-      static_cast<uint16_t*>(out)[i] = uint16_t(pack_bf16x2_rne(v, 0.f));
-    else
-      static_cast<float*>(out)[i] = v;
-  };
-  const float* src = z < 2 ? partial + size_t(z) * C * Fp : partial_g;
+  const bool bias = z == 2 && gb && blockIdx.y == 0;
+  if (!out && !bias) return;
+  const float* src = (z < 2 ? partial + size_t(z) * C * Fp : partial_g) + f;
   const size_t step = z < 2 ? size_t(2) * C * Fp : size_t(C + 1) * Fp;
   const int n = z < 2 ? S : Sg;
-  if (out) {
+  float v[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = k; p < n; p += 8) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int c = c0 + r8 + 8 * k, f = f0 + col;
-      float v = 0.f;
-      if (c < C)
-        for (int p = 0; p < n; ++p) v += src[p * step + size_t(c) * Fp + f];
-      if (z == 0)
-        tile[r8 + 8 * k][col] = v;
-      else if (c < C && f < F)
-        put(size_t(c) * F + f, v);
-    }
-    if (z == 0) {
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = c0 + col, f = f0 + r8 + 8 * k;
-        if (c < C && f < F) put(size_t(f) * C + c, tile[col][r8 + 8 * k]);
-      }
-    }
+    for (int i = 0; i < 4; ++i) v[i] += src[p * step + size_t(c0 + i) * Fp];
+    if (bias) v[4] += src[p * step + size_t(C) * Fp];
   }
-  if (z == 2 && gb && blockIdx.y == 0 && r8 == 0 && f0 + col < F) {
-    float v = 0.f;
-    for (int p = 0; p < n; ++p) v += src[p * step + size_t(C) * Fp + f0 + col];
-    gb[f0 + col] = v;
+#pragma unroll
+  for (int i = 0; i < 5; ++i) red[k][i][col] = v[i];
+  __syncthreads();
+  if (k >= 5 || f >= F) return;
+  float t = red[0][k][col];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) t += red[j][k][col];
+  if (k == 4) {
+    if (bias) gb[f] = t;
+  } else if (out) {
+    const size_t at = z == 0 ? size_t(f) * C + c0 + k : size_t(c0 + k) * F + f;
+    if constexpr (BF)
+      static_cast<uint16_t*>(out)[at] = uint16_t(pack_bf16x2_rne(t, 0.f));
+    else
+      static_cast<float*>(out)[at] = t;
   }
 }
 
@@ -859,7 +867,7 @@ Layout layout(const FfnShape& p, bool backward) {
     l.r0 = o;
     o += al256(size_t(p.N) * p.C * 4);
     // one workgroup a CU over the ranges of rows; a range has a node at least
-    const int per = 2 * wgrad_tiles(l.CT, p.bf16), fb = (l.FT + per - 1) / per;
+    const int per = wgrad_waves(l.CT, p.bf16) / 2, fb = (l.FT + per - 1) / per;
     const int most = device_cus() / fb;
     l.S = p.N < most ? p.N : (most > 1 ? most : 1);
     if (l.S < 1) l.S = 1;
@@ -984,8 +992,8 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
     auto k = k_ffn_wgrad<CT, BF>;
     e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     if (e != hipSuccess) return e;
-    const int per = 2 * wgrad_tiles(CT, BF);
-    k<<<dim3((l.FT + per - 1) / per, l.S), dim3(256), lds, s>>>(w);
+    const int per = wgrad_waves(CT, BF) / 2;
+    k<<<dim3((l.FT + per - 1) / per, l.S), dim3(wgrad_waves(CT, BF) * kWave), lds, s>>>(w);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -996,7 +1004,7 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (a.grad_w_up || a.grad_w_down || a.grad_w_gate || a.grad_b_gate) {
-    k_ffn_wsum<BF><<<dim3(l.FT, l.CT, 3), dim3(256), 0, s>>>(p.C, p.F, l.FT, l.S, l.Sg, w.partial, part_g,
+    k_ffn_wsum<BF><<<dim3(l.FT, p.C / 4, 3), dim3(256), 0, s>>>(p.C, p.F, l.FT, l.S, l.Sg, w.partial, part_g,
                                                              a.grad_w_down, a.grad_w_up, a.grad_w_gate, a.grad_b_gate);
     e = hipGetLastError();
     if (e != hipSuccess) return e;

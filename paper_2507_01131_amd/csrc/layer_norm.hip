@@ -231,8 +231,18 @@ __global__ __launch_bounds__(1024) void k_norm_sum(int n_part, int n, int n_gamm
   __shared__ float red[16][64];
   const int col = threadIdx.x & 63, k = threadIdx.x >> 6, i = blockIdx.x * 64 + col;
   float s = 0.f;
-  if (i < n)
-    for (int p = k; p < n_part; p += 16) s += partial[size_t(p) * n + i];
+  if (i < n) {
+    // eight loads in flight, added in order
+    int p = k;
+    for (; p + 7 * 16 < n_part; p += 8 * 16) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = partial[size_t(p + 16 * u) * n + i];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; p < n_part; p += 16) s += partial[size_t(p) * n + i];
+  }
   red[k][col] = s;
   __syncthreads();
   if (k == 0 && i < n) {
