@@ -24,8 +24,10 @@
 // their largest magnitudes, the packed weights per tile of F, and the second
 // product's operand by a running exponent per row (per hidden unit in
 // k_ffn_wgrad) that only grows; the sums are rescaled when it does.  bf16
-// problems: 32x32x16 bf16 MFMA; h, dh s and dq are rounded to bf16 once, as
-// operands; u, dh, q, s and all sums stay fp32.
+// problems: 32x32x16 bf16 MFMA; h, dh s and (for grad_x) dq are rounded to bf16
+// once, as operands; u, dh, q, s and all sums stay fp32.
+#include <algorithm>
+
 #include "common.hpp"
 #include "kernels.h"
 
@@ -38,6 +40,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlk = 64;  // u32x4 words of an operand block: 64 lanes x 8 values of 16 bits
+constexpr int kMaxFfnTiles = 128;  // F <= 4096
 constexpr int kUnset = -1000;  // exponent of a sum that holds nothing yet
 
 template <bool BF>
@@ -58,7 +61,35 @@ __device__ __forceinline__ f32x16 mm_parts(const u32x4* a, const u32x4* b, f32x1
   }
   return mm<BF>(a[0], b[0], c);
 }
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// the maximum and the sum of a lane's value and its other half's
+__device__ __forceinline__ float halves_max(float v) {
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+// Steps of P operand blocks each, read from LDS kDepth - 1 steps ahead of
+// their matrix instructions: use(step, blocks).
+template <int kSteps, int P, int kDepth, typename Use>
+__device__ __forceinline__ void stream_blocks(const u32x4* w, Use use) {
+  u32x4 ring[kDepth][P];
+#pragma unroll
+  for (int i = 0; i < kDepth - 1 && i < kSteps; ++i)
+#pragma unroll
+    for (int p = 0; p < P; ++p) ring[i][p] = w[(i * P + p) * kBlk];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    if (i + kDepth - 1 < kSteps)
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        ring[(i + kDepth - 1) % kDepth][p] = w[((i + kDepth - 1) * P + p) * kBlk];
+    __builtin_amdgcn_sched_barrier(0);
+    use(i, ring[i % kDepth]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
 
 template <bool BF>
 __device__ __forceinline__ f32x4 load4(const void* p, size_t i) {
@@ -123,7 +154,7 @@ __device__ __forceinline__ int load_row(const void* base, bool on, size_t at, in
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fabsf(v[st][k][i]));
       }
-    mx = fmaxf(mx, other_half(mx));
+    mx = halves_max(mx);
     const int e = f16_split_exponent(mx);
     const float sc = ldexpf(1.f, -e);
 #pragma unroll
@@ -139,23 +170,20 @@ __device__ __forceinline__ int load_row(const void* base, bool on, size_t at, in
   }
 }
 
-// Sixteen accumulator values of a lane's column as the second product's
-// operand (two K-steps).  fp32 problems: scaled by 2^-(E - bias), E the
-// column's running exponent, with `grow` called on the factor that takes the
-// column's sums to a larger E.
+// Sixteen accumulator values of a lane's column become the second product's
+// operand (two K-steps of eight values).  fp32 problems: scaled by 2^-(E -
+// bias), E the column's running exponent.  operand_scale raises E where the
+// column needs it, calling `grow` on the factor that takes the column's sums
+// along, and returns the scale; operand_pair converts values 2 i and 2 i + 1.
 template <bool BF, typename Grow>
-__device__ __forceinline__ void to_operand(const float (&t)[16], int bias, int& E, u32x4 (&op)[2][BF ? 1 : 2],
-                                           Grow grow) {
+__device__ __forceinline__ float operand_scale(const float (&t)[16], int bias, int& E, Grow grow) {
   if constexpr (BF) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) op[q][0][k] = pack_bf16x2_rne(t[8 * q + 2 * k], t[8 * q + 2 * k + 1]);
+    return 1.f;
   } else {
     float mx = 0.f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) mx = fmaxf(mx, fabsf(t[v]));
-    mx = fmaxf(mx, other_half(mx));
+    mx = halves_max(mx);
     const int e = f16_split_exponent(mx) + bias;
     const bool up = mx > 0.f && e > E;
     if (__any(up)) {
@@ -164,17 +192,26 @@ __device__ __forceinline__ void to_operand(const float (&t)[16], int bias, int& 
       E = to;
     }
     // (a column of zeros may come before its exponent is set)
-    const float sc = ldexpf(1.f, min(bias - E, 126));
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t hi, lo;
-        split_f16x2_pair(t[8 * q + 2 * k] * sc, t[8 * q + 2 * k + 1] * sc, hi, lo);
-        op[q][0][k] = hi;
-        op[q][1][k] = lo;
-      }
+    return ldexpf(1.f, min(bias - E, 126));
   }
+}
+template <bool BF>
+__device__ __forceinline__ void operand_pair(const float (&t)[16], float sc, int i, u32x4 (&op)[2][BF ? 1 : 2]) {
+  if constexpr (BF) {
+    op[i >> 2][0][i & 3] = pack_bf16x2_rne(t[2 * i], t[2 * i + 1]);
+  } else {
+    uint32_t hi, lo;
+    split_f16x2_pair(t[2 * i] * sc, t[2 * i + 1] * sc, hi, lo);
+    op[i >> 2][0][i & 3] = hi;
+    op[i >> 2][1][i & 3] = lo;
+  }
+}
+template <bool BF, typename Grow>
+__device__ __forceinline__ void to_operand(const float (&t)[16], int bias, int& E, u32x4 (&op)[2][BF ? 1 : 2],
+                                           Grow grow) {
+  const float sc = operand_scale<BF>(t, bias, E, grow);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) operand_pair<BF>(t, sc, i, op);
 }
 
 // ------------------------------------------------------------------ weights
@@ -192,15 +229,17 @@ struct PackArgs {
   int n;
 };
 
+constexpr int kPackThreads = 1024;
 template <bool BF>
-__global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a, int C, int F, int CT) {
+__global__ __launch_bounds__(kPackThreads) void k_ffn_pack(PackArgs a, int C, int F, int CT) {
   extern __shared__ float tile[];  // [32][32 CT + 1]
-  __shared__ float red[4];
+  __shared__ float red[kPackThreads / kWave];
   constexpr int P = BF ? 1 : 2;
   const int ft = blockIdx.x, j = blockIdx.y, tid = threadIdx.x;
   const int Cp = 32 * CT, ld = Cp + 1, sc = a.sc[j], sf = a.sf[j];
   float mx = 0.f;
-  for (int i = tid; i < 32 * Cp; i += 256) {
+#pragma unroll 4
+  for (int i = tid; i < 32 * Cp; i += kPackThreads) {
     // the index with stride 1 runs over the lanes
     const int f = sf == 1 ? i & 31 : i / Cp, c = sf == 1 ? i >> 5 : i - (i / Cp) * Cp;
     const bool ok = c < C && 32 * ft + f < F;
@@ -218,12 +257,14 @@ __global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a, int C, int F, int 
   }
   __syncthreads();
   if constexpr (!BF) {
-    const int e = f16_split_exponent(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+#pragma unroll
+    for (int w = 0; w < kPackThreads / kWave; ++w) mx = fmaxf(mx, red[w]);
+    const int e = f16_split_exponent(mx);
     scale = ldexpf(1.f, -e);
     if (tid == 0) a.e[j][ft] = e;
   }
   u32x4* out = a.out[j] + size_t(ft) * 2 * CT * P * kBlk;
-  for (int i = tid; i < 2 * CT * kBlk; i += 256) {
+  for (int i = tid; i < 2 * CT * kBlk; i += kPackThreads) {
     const int blk = i / kBlk, ln = i & 63, h = ln >> 5, l32 = ln & 31;
     u32x4 w[P];
 #pragma unroll
@@ -248,23 +289,60 @@ __global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a, int C, int F, int 
 }
 
 // --------------------------------------------------------------------- gate
-// s = act(q) and, if asked for, act'(q), [N, 32 FT] fp32 each: a wave takes 32
-// nodes (lanes) and kGateTiles tiles of hidden units.
+// Operand blocks of the packed weights into LDS by direct loads: this wave's
+// `n` of a run of 4 n blocks of 1 KB.
+template <int n>
+__device__ __forceinline__ void blocks_to_lds(const u32x4* src, u32x4* dst, int wave, int lane) {
+#pragma unroll
+  for (int k = 0; k < n; ++k)
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(src + (wave * n + k) * kBlk + lane),
+        (__attribute__((address_space(3))) void*)(dst + (wave * n + k) * kBlk), 16, 0, 0);
+}
+// every wave's direct loads are in LDS
+__device__ __forceinline__ void lds_loads_done() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  __syncthreads();
+}
+
+// s = act(q) and, if asked for, act'(q), [N, 32 FT] fp32 each: a workgroup
+// takes 128 nodes (lanes) and two tiles of hidden units.
 constexpr int kGateTiles = 2;
 template <int CT, bool BF>
 __global__ __launch_bounds__(256) void k_ffn_gate(int N, int d, int C, int F, int FT, int act,
                                                   const void* __restrict__ x, const u32x4* __restrict__ wg,
                                                   const int* __restrict__ eg, const float* __restrict__ b,
                                                   float* __restrict__ s, float* __restrict__ ds) {
-  constexpr int P = BF ? 1 : 2;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, l32 = lane & 31;
+  constexpr int P = BF ? 1 : 2, kHalf = 2 * CT * P * kBlk;
+  extern __shared__ u32x4 sw[];  // [kGateTiles][kHalf]
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = (blockIdx.x * 4 + wave) * kTile + l32;
-  if (n - l32 >= N) return;
+  const int f0 = blockIdx.y * kGateTiles, tiles = min(kGateTiles, FT - f0);
+  if constexpr (CT * P % 2 == 0) {
+#pragma unroll
+    for (int t = 0; t < kGateTiles; ++t)
+      if (t < tiles)
+        blocks_to_lds<CT * P / 2>(wg + size_t(f0 + t) * kHalf, sw + t * kHalf, wave, lane);
+  } else {
+    for (int i = threadIdx.x; i < tiles * kHalf; i += 256) sw[i] = wg[size_t(f0) * kHalf + i];
+  }
   u32x4 xo[2 * CT][P];
   const int ex = load_row<CT, BF>(x, n < N, n < N ? size_t(n) * d * C : 0, C, h, xo);
-  for (int ft = blockIdx.y * kGateTiles; ft < min(FT, int(blockIdx.y + 1) * kGateTiles); ++ft) {
+  f32x4 bias[kGateTiles][4];
+#pragma unroll
+  for (int t = 0; t < kGateTiles; ++t)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int f = 32 * (f0 + t) + 8 * k + 4 * h;  // (F is a multiple of 16: a quad is inside or outside)
+      bias[t][k] = b && f < F ? *reinterpret_cast<const f32x4*>(b + f) : f32x4{};
+    }
+  lds_loads_done();
+#pragma unroll
+  for (int t = 0; t < kGateTiles; ++t) {
+    if (t >= tiles) break;
     f32x16 acc = f32x16{};
-    const u32x4* w = wg + size_t(ft) * 2 * CT * P * kBlk + lane;
+    const u32x4* w = sw + t * kHalf + lane;
 #pragma unroll
     for (int st = 0; st < 2 * CT; ++st) {
       u32x4 a[P];
@@ -272,19 +350,18 @@ __global__ __launch_bounds__(256) void k_ffn_gate(int N, int d, int C, int F, in
       for (int p = 0; p < P; ++p) a[p] = w[(st * P + p) * kBlk];
       acc = mm_parts<BF>(a, xo[st], acc);
     }
-    const int e = BF ? 0 : ex + eg[ft];
+    const int e = BF ? 0 : ex + eg[f0 + t];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int f = 32 * ft + 8 * k + 4 * h;
-      f32x4 sv = f32x4{}, dv = f32x4{};
+      const int f = 32 * (f0 + t) + 8 * k + 4 * h;
+      f32x4 sv, dv;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (f < F) {  // (F is a multiple of 16: a quad is inside or outside)
-          float s1, d1;
-          gate_act((BF ? acc[4 * k + i] : ldexpf(acc[4 * k + i], e)) + (b ? b[f + i] : 0.f), act, s1, d1);
-          sv[i] = s1;
-          dv[i] = d1;
-        }
+      for (int i = 0; i < 4; ++i) {
+        float s1, d1;
+        gate_act((BF ? acc[4 * k + i] : ldexpf(acc[4 * k + i], e)) + bias[t][k][i], act, s1, d1);
+        sv[i] = f < F ? s1 : 0.f;
+        dv[i] = f < F ? d1 : 0.f;
+      }
       if (n < N) {
         *reinterpret_cast<f32x4*>(s + size_t(n) * 32 * FT + f) = sv;
         if (ds) *reinterpret_cast<f32x4*>(ds + size_t(n) * 32 * FT + f) = dv;
@@ -301,36 +378,49 @@ struct RowsArgs {
   const int *e_up, *e_down;  // their exponents (fp32 problems)
   const float* s;            // [M / d, 32 FT]
   const void* residual;      // [M, C] of the problem's type, or nullptr
-  const float* residual0;    // [M / d, C], added to the degree-0 rows, or nullptr
+  const float* residual0;    // [n_res0, M / d, C], added to the degree-0 rows, or nullptr
+  int n_res0;
   void* out;                 // [M, C]
 };
 
-// A workgroup takes 4 x 32 NB rows.  The packed weights of one tile of F come
-// into LDS by direct loads while the tile before is used.
+// Waves a SIMD: two where a wave's rows and sums leave room in 256 registers.
+__host__ __device__ constexpr int rows_waves(int CT, bool BF, int NB) {
+  return NB * CT * (BF ? 24 : 32) <= 128 ? 2 : 1;
+}
+
+// A workgroup takes 4 x 32 NB rows.  The packed weights come into LDS by
+// direct loads one tile of F ahead of their use, and u of the next tile is
+// formed beside the conversion of this tile's h, so that neither the loads
+// nor the vector work stand between the matrix instructions.
 template <int CT, bool BF, int NB>
-__global__ __launch_bounds__(256) void k_ffn_rows(RowsArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(CT, BF, NB)))) void k_ffn_rows(
+    RowsArgs a) {
   constexpr int P = BF ? 1 : 2;
   constexpr int kHalf = 2 * CT * P * kBlk;  // words of a tile's up (and down) operands
-  extern __shared__ u32x4 sw[];             // [2][2 kHalf]
+  constexpr int kWaves = rows_waves(CT, BF, NB), kDepth = kWaves == 2 ? 3 : 4;
+  constexpr int kChains = kWaves == 2 || NB > 1 ? 1 : 2;  // of a row tile's u
+  extern __shared__ u32x4 sw[];                           // up [2][kHalf], down [2][kHalf]
+  __shared__ int s_bias[kMaxFfnTiles];                    // the tiles' exponents, of both weights
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int C = a.C, FT = a.FT;
-  auto fetch = [&](int ft, int buf) {
-#pragma unroll
-    for (int k = 0; k < CT * P; ++k) {
-      const int blk = wave * CT * P + k;  // of 4 CT P: the up operands, then the down operands
-      const u32x4* src = (blk < 2 * CT * P ? a.up + size_t(ft) * kHalf + blk * kBlk
-                                           : a.down + size_t(ft) * kHalf + (blk - 2 * CT * P) * kBlk) + lane;
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)src,
-          (__attribute__((address_space(3))) void*)(sw + buf * 2 * kHalf + blk * kBlk), 16, 0, 0);
-    }
+  auto fetch = [&](const u32x4* packed, int ft, int buf) {
+    const u32x4* src = packed + size_t(ft) * kHalf;
+    u32x4* dst = sw + buf * kHalf;
+    blocks_to_lds<CT * P / 2>(src, dst, wave, lane);
+    if constexpr (CT * P % 2 == 1)  // an odd pair of blocks is left
+      if (wave < 2) blocks_to_lds<1>(src + 4 * (CT * P / 2) * kBlk, dst + 4 * (CT * P / 2) * kBlk, wave, lane);
   };
-  fetch(0, 0);
+  fetch(a.up, 0, 0);
+  if (FT > 1) fetch(a.up, 1, 1);
+  fetch(a.down, 0, 2);
+  if constexpr (!BF)
+    for (int i = threadIdx.x; i < FT; i += 256) s_bias[i] = a.e_up[i] + a.e_down[i];
   int row[NB], ex[NB], E[NB];
   const float* s[NB];
   u32x4 xo[NB][2 * CT][P];
-  f32x16 y[NB][CT];
+  f32x16 y[NB][CT], u[NB];
+  f32x4 sv[NB][4];
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     row[b] = (blockIdx.x * 4 + wave) * (kTile * NB) + b * kTile + l32;
@@ -338,177 +428,257 @@ __global__ __launch_bounds__(256) void k_ffn_rows(RowsArgs a) {
     const int r = on ? row[b] : a.M - 1;
     ex[b] = load_row<CT, BF>(a.in, on, size_t(r) * C, C, h, xo[b]);
     s[b] = a.s + size_t(r / a.d) * 32 * FT + 4 * h;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 8 * k);
     E[b] = kUnset;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) y[b][ct] = f32x16{};
   }
-  for (int ft = 0; ft < FT; ++ft) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share of the tile's weights is in LDS
-    __syncthreads();                     // every wave's is; the other buffer is free
-    if (ft + 1 < FT) fetch(ft + 1, (ft + 1) & 1);
-    const u32x4* w = sw + (ft & 1) * 2 * kHalf + lane;
-    f32x4 sv[NB][4];
+  // u of one tile; beside(i) is the vector work that goes with step i
+  auto up_product = [&](int buf, auto beside) {
+    f32x16 c[NB][kChains];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 32 * ft + 8 * k);
-    f32x16 u[NB];
+      for (int k = 0; k < kChains; ++k) c[b][k] = f32x16{};
+    stream_blocks<2 * CT, P, kDepth>(sw + buf * kHalf + lane, [&](int st, const u32x4* wa) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) u[b] = f32x16{};
+      for (int b = 0; b < NB; ++b) c[b][st % kChains] = mm_parts<BF>(wa, xo[b][st], c[b][st % kChains]);
+      beside(st);
+    });
 #pragma unroll
-    for (int st = 0; st < 2 * CT; ++st) {
-      u32x4 wa[P];
-#pragma unroll
-      for (int p = 0; p < P; ++p) wa[p] = w[(st * P + p) * kBlk];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) u[b] = mm_parts<BF>(wa, xo[b][st], u[b]);
-    }
+    for (int b = 0; b < NB; ++b) u[b] = kChains == 2 ? c[b][0] + c[b][kChains - 1] : c[b][0];
+  };
+  lds_loads_done();
+  up_product(0, [](int) {});
+  for (int ft = 0; ft < FT; ++ft) {
+    lds_loads_done();  // W_up of tile ft + 1 and W_down of tile ft; the buffers used before are free
+    if (ft + 2 < FT) fetch(a.up, ft + 2, ft & 1);
+    if (ft + 1 < FT) fetch(a.down, ft + 1, 2 + ((ft + 1) & 1));
+    const int bias = BF ? 0 : s_bias[ft];
     u32x4 ho[NB][2][P];
-    const int bias = BF ? 0 : a.e_up[ft] + a.e_down[ft];
+    float t[NB][16], sc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      float t[16];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) t[v] = u[b][v] * sv[b][v >> 2][v & 3];
-      to_operand<BF>(t, bias, E[b], ho[b], [&](float f) {
+      for (int v = 0; v < 16; ++v) t[b][v] = u[b][v] * sv[b][v >> 2][v & 3];
+      sc[b] = operand_scale<BF>(t[b], bias, E[b], [&](float f) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) y[b][ct] *= f;
       });
     }
+    // the pairs of h, spread over the steps of the next tile's u
+    auto convert = [&](int st) {
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32x4 wa[P];
+        for (int i = 0; i < 8; ++i)
+          if (i * 2 * CT / 8 == st) operand_pair<BF>(t[b], sc[b], i, ho[b]);
+    };
+    if (ft + 1 < FT) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) wa[p] = w[kHalf + ((2 * ct + q) * P + p) * kBlk];
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int b = 0; b < NB; ++b) y[b][ct] = mm_parts<BF>(wa, ho[b][q], y[b][ct]);
-      }
+        for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 32 * (ft + 1) + 8 * k);
+      up_product((ft + 1) & 1, convert);
+    } else {
+#pragma unroll
+      for (int st = 0; st < 2 * CT; ++st) convert(st);
+    }
+    stream_blocks<2 * CT, P, kDepth>(sw + (2 + (ft & 1)) * kHalf + lane, [&](int i, const u32x4* wa) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) y[b][i >> 1] = mm_parts<BF>(wa, ho[b][i & 1], y[b][i >> 1]);
+    });
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     if (row[b] >= a.M) continue;
     const int e = BF ? 0 : E[b] + ex[b];
     const int n = row[b] / a.d;
-    const bool first = a.residual0 && n * a.d == row[b];
+    if constexpr (!BF)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) y[b][ct][v] = ldexpf(y[b][ct][v], e);
+    if (a.residual0 && n * a.d == row[b])
+      for (int p = 0; p < a.n_res0; ++p) {
+        const float* r0 = a.residual0 + (size_t(p) * (a.M / a.d) + n) * C + 4 * h;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const f32x4 r = 32 * ct + 8 * k < C ? *reinterpret_cast<const f32x4*>(r0 + 32 * ct + 8 * k) : f32x4{};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[b][ct][4 * k + i] += r[i];
+          }
+      }
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int c = 32 * ct + 8 * k + 4 * h;
         if (c >= C) continue;
-        f32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = BF ? y[b][ct][4 * k + i] : ldexpf(y[b][ct][4 * k + i], e);
+        f32x4 v{y[b][ct][4 * k], y[b][ct][4 * k + 1], y[b][ct][4 * k + 2], y[b][ct][4 * k + 3]};
         if (a.residual) v += load4<BF>(a.residual, size_t(row[b]) * C + c);
-        if (first) v += *reinterpret_cast<const f32x4*>(a.residual0 + size_t(n) * C + c);
         store4<BF>(a.out, size_t(row[b]) * C + c, v);
       }
   }
 }
 
 // ------------------------------------------------------ the gate's gradients
-// r0 = dq W_gate^T [N, C]: a workgroup takes 32 nodes, each wave every fourth
-// tile of channels.
+// r0 = dq W_gate^T, the sums over gridDim.y shares of F apart: [gridDim.y, N, C].
+// A workgroup takes 128 nodes; the packed weights go through LDS as in
+// k_ffn_rows.
 template <int CT, bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const float* __restrict__ dq,
                                                  const u32x4* __restrict__ wg, const int* __restrict__ eg,
                                                  float* __restrict__ r0) {
-  constexpr int P = BF ? 1 : 2;
-  constexpr int T = (CT + 3) / 4;
+  constexpr int P = BF ? 1 : 2, kHalf = 2 * CT * P * kBlk;
+  extern __shared__ u32x4 sw[];  // [2][kHalf]
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = blockIdx.x * kTile + l32;
+  const int n = (blockIdx.x * 4 + wave) * kTile + l32;
+  const int f0 = blockIdx.y * FT / gridDim.y, f1 = (blockIdx.y + 1) * FT / gridDim.y;
   const float* q = dq + size_t(min(n, N - 1)) * 32 * FT + 4 * h;
-  f32x16 acc[T];
+  auto fetch = [&](int ft, int buf) {
+    const u32x4* src = wg + size_t(ft) * kHalf;
+    u32x4* dst = sw + buf * kHalf;
+    blocks_to_lds<CT * P / 2>(src, dst, wave, lane);
+    if constexpr (CT * P % 2 == 1)
+      if (wave < 2) blocks_to_lds<1>(src + 4 * (CT * P / 2) * kBlk, dst + 4 * (CT * P / 2) * kBlk, wave, lane);
+  };
+  fetch(f0, 0);
+  f32x4 dv[4];
 #pragma unroll
-  for (int t = 0; t < T; ++t) acc[t] = f32x16{};
+  for (int k = 0; k < 4; ++k) dv[k] = *reinterpret_cast<const f32x4*>(q + 32 * f0 + 8 * k);
+  f32x16 acc[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x16{};
   int E = kUnset;
-  for (int ft = 0; ft < FT; ++ft) {
+  for (int ft = f0; ft < f1; ++ft) {
+    lds_loads_done();
+    if (ft + 1 < f1) fetch(ft + 1, (ft + 1 - f0) & 1);
     float t[16];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(q + 32 * ft + 8 * k);
+    for (int v = 0; v < 16; ++v) t[v] = dv[v >> 2][v & 3];
+    if (ft + 1 < f1)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) t[4 * k + i] = v[i];
-    }
+      for (int k = 0; k < 4; ++k) dv[k] = *reinterpret_cast<const f32x4*>(q + 32 * (ft + 1) + 8 * k);
     u32x4 o[2][P];
     to_operand<BF>(t, BF ? 0 : eg[ft], E, o, [&](float f) {
 #pragma unroll
-      for (int j = 0; j < T; ++j) acc[j] *= f;
+      for (int ct = 0; ct < CT; ++ct) acc[ct] *= f;
     });
+    const u32x4* w = sw + ((ft - f0) & 1) * kHalf + lane;
 #pragma unroll
-    for (int j = 0; j < T; ++j) {
-      const int ct = wave + 4 * j;
-      if (ct >= CT) break;
+    for (int qq = 0; qq < 2; ++qq)
 #pragma unroll
-      for (int qq = 0; qq < 2; ++qq) {
-        u32x4 w[P];
+      for (int ct = 0; ct < CT; ++ct) {
+        u32x4 wa[P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) w[p] = wg[((size_t(ft) * CT + ct) * 2 + qq) * P * kBlk + p * kBlk + lane];
-        acc[j] = mm_parts<BF>(w, o[qq], acc[j]);
+        for (int p = 0; p < P; ++p) wa[p] = w[((2 * ct + qq) * P + p) * kBlk];
+        acc[ct] = mm_parts<BF>(wa, o[qq], acc[ct]);
       }
-    }
   }
   if (n >= N) return;
 #pragma unroll
-  for (int j = 0; j < T; ++j) {
-    const int ct = wave + 4 * j;
-    if (ct >= CT) break;
+  for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int c = 32 * ct + 8 * k + 4 * h;
       if (c >= C) continue;
       f32x4 v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = BF ? acc[j][4 * k + i] : ldexpf(acc[j][4 * k + i], E);
-      *reinterpret_cast<f32x4*>(r0 + size_t(n) * C + c) = v;
+      for (int i = 0; i < 4; ++i) v[i] = BF ? acc[ct][4 * k + i] : ldexpf(acc[ct][4 * k + i], E);
+      *reinterpret_cast<f32x4*>(r0 + (size_t(blockIdx.y) * N + n) * C + c) = v;
     }
-  }
 }
 
-// grad W_gate = x[:, 0]^T dq in 32x32x2 fp32 MFMA, one tile of 32 x 32 a wave
-// over a range of nodes; the waves of the first channel tile also sum dq
-// (grad b).  partial [S][C + 1][32 FT]: the last row is grad b.
+// grad W_gate = x[:, 0]^T dq: a wave takes 32 channels and two tiles of hidden
+// units over a range of nodes, sixteen nodes a step with the next step's loads
+// in flight; 32x32x2 fp32 MFMA, or 32x32x16 bf16 MFMA over three bf16 parts of
+// dq (to 2^-24: nothing of it is rounded away).  The waves of the first channel tile also sum dq (grad b).  partial [S][C + 1]
+// [32 FT]: the last row is grad b.
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, int FT, const void* __restrict__ x,
                                                  const float* __restrict__ dq, float* __restrict__ partial) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, l32 = lane & 31;
-  const int t = blockIdx.x * 4 + wave;
-  if (t >= CT * FT) return;
-  const int ct = t / FT, ft = t - ct * FT, c = 32 * ct + l32, f = 32 * ft + l32;
+  const int FP = (FT + 1) / 2, t = blockIdx.x * 4 + wave;
+  if (t >= CT * FP) return;
+  const int ct = t / FP, ft = 2 * (t - ct * FP), c = 32 * ct + l32, Fp = 32 * FT;
   const int n0 = int(int64_t(blockIdx.y) * N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * N / gridDim.y);
-  f32x16 acc = f32x16{};
-  float sum = 0.f;
-  auto at = [&](int n) {
-    if constexpr (BF)
-      return bf16_to_f32(static_cast<const uint16_t*>(x)[size_t(n) * d * C + c]);
-    else
-      return static_cast<const float*>(x)[size_t(n) * d * C + c];
+  const bool two = ft + 1 < FT;
+  f32x16 acc[2] = {f32x16{}, f32x16{}};
+  float sum[2] = {0.f, 0.f};
+  struct Step {
+    float b[2][8];
+    float a[8];
+    uint16_t ab[8];
   };
+  // value k of a lane: node 8 h + k (bf16: the K order of the step) or 2 k + h
+  auto load = [&](int n, Step& s) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int nn = n + (BF ? 8 * h + k : 2 * k + h);
+      const bool on = nn < n1;
+      const size_t at = size_t(on ? nn : n0);
+      if constexpr (BF)
+        s.ab[k] = on && c < C ? static_cast<const uint16_t*>(x)[at * d * C + c] : uint16_t(0);
+      else
+        s.a[k] = on && c < C ? static_cast<const float*>(x)[at * d * C + c] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) s.b[j][k] = on && (j == 0 || two) ? dq[at * Fp + 32 * (ft + j) + l32] : 0.f;
+    }
+  };
+  Step cur, nxt;
+  load(n0, cur);
   for (int n = n0; n < n1; n += 16) {
-    float av[8], bv[8];
+    if (n + 16 < n1) load(n + 16, nxt);
+    if constexpr (BF) {
+      u32x4 av;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int nn = n + 2 * k + h;
-      av[k] = nn < n1 && c < C ? at(nn) : 0.f;
-      bv[k] = nn < n1 ? dq[size_t(nn) * 32 * FT + f] : 0.f;
+      for (int k = 0; k < 4; ++k) av[k] = uint32_t(cur.ab[2 * k]) | uint32_t(cur.ab[2 * k + 1]) << 16;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float rest[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) rest[k] = cur.b[j][k];
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          u32x4 bv;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            bv[k] = pack_bf16x2_rne(rest[2 * k], rest[2 * k + 1]);
+            rest[2 * k] -= __uint_as_float(bv[k] << 16);
+            rest[2 * k + 1] -= __uint_as_float(bv[k] & 0xffff0000u);
+          }
+          acc[j] = mm<true>(av, bv, acc[j]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[j] = mfma32(cur.a[k], cur.b[j][k], acc[j]);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      acc = mfma32(av[k], bv[k], acc);
-      sum += bv[k];
-    }
-  }
-  float* out = partial + size_t(blockIdx.y) * (C + 1) * 32 * FT + f;
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int cc = 32 * ct + acc_row(v, h);
-    if (cc < C) out[size_t(cc) * 32 * FT] = acc[v];
+      for (int k = 0; k < 8; ++k) sum[j] += cur.b[j][k];
+    cur = nxt;
   }
-  sum += other_half(sum);
-  if (ct == 0 && h == 0) out[size_t(C) * 32 * FT] = sum;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (j == 1 && !two) break;
+    float* out = partial + size_t(blockIdx.y) * (C + 1) * Fp + 32 * (ft + j) + l32;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int cc = 32 * ct + acc_row(v, h);
+      if (cc < C) out[size_t(cc) * Fp] = acc[j][v];
+    }
+    sum[j] = halves_sum(sum[j]);
+    if (ct == 0 && h == 0) out[size_t(C) * Fp] = sum[j];
+  }
 }
 
 // ------------------------------------------------------- weights' gradients
@@ -838,7 +1008,7 @@ size_t al256(size_t b) { return (b + 255) & ~size_t(255); }
 
 struct Layout {
   size_t pack[5], exps, s, ds, dq, r0, part, part_g, total;
-  int CT, FT, P, S, Sg;
+  int CT, FT, P, S, Sg, KS;
   size_t pack_bytes;
 };
 // packs: up, down, gate (forward); W_up and W_down^T as up, W_up^T as down,
@@ -865,7 +1035,9 @@ Layout layout(const FfnShape& p, bool backward) {
     l.dq = o;
     o += gate;
     l.r0 = o;
-    o += al256(size_t(p.N) * p.C * 4);
+    // shares of F, so that there is a workgroup a CU
+    l.KS = std::min({4, l.FT, std::max(1, device_cus() / ((p.N + 127) / 128 + 1))});
+    o += al256(size_t(l.KS) * p.N * p.C * 4);
     // one workgroup a CU over the ranges of rows; a range has a node at least
     const int per = wgrad_waves(l.CT, p.bf16) / 2, fb = (l.FT + per - 1) / per;
     const int most = device_cus() / fb;
@@ -873,7 +1045,7 @@ Layout layout(const FfnShape& p, bool backward) {
     if (l.S < 1) l.S = 1;
     l.part = o;
     o += al256(size_t(l.S) * 2 * p.C * 32 * l.FT * 4);
-    const int blocks = (l.CT * l.FT + 3) / 4;
+    const int blocks = (l.CT * ((l.FT + 1) / 2) + 3) / 4;
     int sg = 2 * device_cus() / blocks;
     const int cap = (p.N + 63) / 64;  // at least 64 nodes a range
     l.Sg = sg < cap ? sg : cap;
@@ -898,7 +1070,7 @@ void add_pack(PackArgs& a, const Layout& l, char* ws, int slot, const void* W, i
 template <bool BF>
 hipError_t pack(const PackArgs& a, const Layout& l, const FfnShape& p, hipStream_t s) {
   const size_t lds = size_t(32) * (32 * l.CT + 1) * 4;
-  k_ffn_pack<BF><<<dim3(l.FT, a.n), dim3(256), lds, s>>>(a, p.C, p.F, l.CT);
+  k_ffn_pack<BF><<<dim3(l.FT, a.n), dim3(kPackThreads), lds, s>>>(a, p.C, p.F, l.CT);
   return hipGetLastError();
 }
 
@@ -906,7 +1078,11 @@ template <int CT, bool BF>
 hipError_t gate(const Layout& l, const FfnShape& p, const void* x, char* ws, int slot, const float* b, bool slope,
                 hipStream_t s) {
   const dim3 grid((p.N + 127) / 128, (l.FT + kGateTiles - 1) / kGateTiles);
-  k_ffn_gate<CT, BF><<<grid, dim3(256), 0, s>>>(
+  constexpr int lds = kGateTiles * 2 * CT * (BF ? 1 : 2) * kBlk * 16;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_ffn_gate<CT, BF>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  k_ffn_gate<CT, BF><<<grid, dim3(256), lds, s>>>(
       p.N, p.d, p.C, p.F, l.FT, p.act, x, reinterpret_cast<const u32x4*>(ws + l.pack[slot]),
       reinterpret_cast<const int*>(ws + l.exps) + slot * l.FT, b, reinterpret_cast<float*>(ws + l.s),
       slope ? reinterpret_cast<float*>(ws + l.ds) : nullptr);
@@ -999,7 +1175,8 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   }
   float* part_g = reinterpret_cast<float*>(ws + l.part_g);
   if (a.grad_w_gate || a.grad_b_gate) {
-    k_ffn_dwg<BF><<<dim3((l.CT * l.FT + 3) / 4, l.Sg), dim3(256), 0, s>>>(p.N, p.d, p.C, l.CT, l.FT, a.x, dq, part_g);
+    k_ffn_dwg<BF><<<dim3((l.CT * ((l.FT + 1) / 2) + 3) / 4, l.Sg), dim3(256), 0, s>>>(p.N, p.d, p.C, l.CT, l.FT, a.x,
+                                                                                     dq, part_g);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -1011,7 +1188,11 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   }
   if (!a.grad_x) return hipSuccess;
   float* r0 = reinterpret_cast<float*>(ws + l.r0);
-  k_ffn_dx0<CT, BF><<<dim3((p.N + 31) / 32), dim3(256), 0, s>>>(
+  constexpr int lds = 2 * 2 * CT * (BF ? 1 : 2) * kBlk * 16;
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_ffn_dx0<CT, BF>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                          lds);
+  if (e != hipSuccess) return e;
+  k_ffn_dx0<CT, BF><<<dim3((p.N + 127) / 128, l.KS), dim3(256), lds, s>>>(
       p.N, p.C, l.FT, dq, reinterpret_cast<const u32x4*>(ws + l.pack[4]), ex + 4 * l.FT, r0);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -1027,6 +1208,7 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   r.e_down = ex + 2 * l.FT;
   r.s = w.s;
   r.residual0 = r0;
+  r.n_res0 = l.KS;
   r.out = a.grad_x;
   return rows<CT, BF>(r, s);
 }
