@@ -385,7 +385,7 @@ struct RowsArgs {
 
 // Waves a SIMD: two where a wave's rows and sums leave room in 256 registers.
 __host__ __device__ constexpr int rows_waves(int CT, bool BF, int NB) {
-  return NB * CT * (BF ? 24 : 32) <= 128 ? 2 : 1;
+  return NB * CT * (BF ? 24 : 32) <= (BF ? 168 : 128) ? 2 : 1;
 }
 
 // A workgroup takes 4 x 32 NB rows.  The packed weights come into LDS by
@@ -476,11 +476,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
           if (i * 2 * CT / 8 == st) operand_pair<BF>(t[b], sc[b], i, ho[b]);
     };
     if (ft + 1 < FT) {
+      up_product((ft + 1) & 1, convert);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 32 * (ft + 1) + 8 * k);
-      up_product((ft + 1) & 1, convert);
     } else {
 #pragma unroll
       for (int st = 0; st < 2 * CT; ++st) convert(st);
@@ -597,8 +597,8 @@ __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const flo
 // grad W_gate = x[:, 0]^T dq: a wave takes 32 channels and two tiles of hidden
 // units over a range of nodes, sixteen nodes a step with the next step's loads
 // in flight; 32x32x2 fp32 MFMA, or 32x32x16 bf16 MFMA over three bf16 parts of
-// dq (to 2^-24: nothing of it is rounded away).  The waves of the first channel tile also sum dq (grad b).  partial [S][C + 1]
-// [32 FT]: the last row is grad b.
+// dq (to 2^-24: nothing of it is rounded away).  The waves of the first channel
+// tile also sum dq (grad b).  partial [S][C + 1][32 FT]: the last row is grad b.
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, int FT, const void* __restrict__ x,
                                                  const float* __restrict__ dq, float* __restrict__ partial) {
