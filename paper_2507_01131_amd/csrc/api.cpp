@@ -665,7 +665,7 @@ size_t packed_bytes(const tdn_problem& p) {
 }
 AttBwdLayout att_bwd_layout(const tdn_problem& p, int H, int F) {
   AttBwdLayout b{};
-  const size_t N = p.n_nodes, E = p.n_edges, ndc = N * dim_of(p.L) * p.C * 4, RT = (p.R + 31) / 32;
+  const size_t N = p.n_nodes, E = p.n_edges, ndc = N * dim_of(p.L) * p.C * 4;
   size_t o = 0;
   auto take = [&](size_t bytes) {
     const size_t at = o;
@@ -690,7 +690,7 @@ AttBwdLayout att_bwd_layout(const tdn_problem& p, int H, int F) {
   b.al_src = take(E * H * 4);
   b.g = take(E * p.R * 4);
   b.dg = take(E * p.R * 4);
-  b.dal = take(RT * E * H * 4);
+  b.dal = take(E * H * 4);
   b.dhid = take(E * F * 4);
   b.dPt = take(N * F * 4);
   b.dPs = take(N * F * 4);

@@ -69,56 +69,71 @@ __global__ __launch_bounds__(256) void k_att_factors(int d, int R, int RT, const
 }
 
 // ---- g_e [E, R] by sorted position: one thread a rank, harmonics and radial
-// basis of 64 edges at a time in LDS.
+// basis of 64 edges at a time in LDS, read sixteen bytes at a time.
 constexpr int kGEdges = 64;
 template <int L>
 __global__ __launch_bounds__(256) void k_att_g(int E, int R, int nr, float sigma, const int32_t* __restrict__ perm,
                                                const float* __restrict__ edge_vec, const float* __restrict__ B,
                                                const float* __restrict__ Wr, float* __restrict__ g) {
-  constexpr int d = (L + 1) * (L + 1);
-  __shared__ float sY[kGEdges][d], sPhi[kGEdges][kMaxRadial];
-  const int r = threadIdx.x, rc = min(r, R - 1);
-  float b[d], w[kMaxRadial];
+  constexpr int d = (L + 1) * (L + 1), dq = (d + 3) / 4;
+  __shared__ f32x4 sY[kGEdges][dq], sPhi[kGEdges][kMaxRadial / 4];
+  const int r = threadIdx.x, rc = min(r, R - 1), nq = (nr + 3) / 4;
+  f32x4 b[dq], w[kMaxRadial / 4];
 #pragma unroll
-  for (int k = 0; k < d; ++k) b[k] = B[k * R + rc];
+  for (int k = 0; k < 4 * dq; ++k) b[k / 4][k % 4] = k < d ? B[k * R + rc] : 0.f;
 #pragma unroll
-  for (int q = 0; q < kMaxRadial; ++q) w[q] = q < nr ? Wr[q * R + rc] : 0.f;
+  for (int q = 0; q < kMaxRadial; ++q) w[q / 4][q % 4] = q < nr ? Wr[q * R + rc] : 0.f;
   const int e0 = blockIdx.x * kGEdges, n = min(kGEdges, E - e0);
   if (int(threadIdx.x) < n) {
     const int eid = perm[e0 + threadIdx.x];
     const float vx = edge_vec[3 * size_t(eid)], vy = edge_vec[3 * size_t(eid) + 1], vz = edge_vec[3 * size_t(eid) + 2];
     const float len = sqrtf(vx * vx + vy * vy + vz * vz), inv = 1.f / len;
-    float Y[d];
+    float Y[4 * dq];
     sh_unit_all<L>(vx * inv, vy * inv, vz * inv, Y);
 #pragma unroll
-    for (int k = 0; k < d; ++k) sY[threadIdx.x][k] = Y[k];
+    for (int k = d; k < 4 * dq; ++k) Y[k] = 0.f;
 #pragma unroll
-    for (int q = 0; q < kMaxRadial; ++q) sPhi[threadIdx.x][q] = radial_phi(len, q, sigma);
+    for (int k = 0; k < dq; ++k) sY[threadIdx.x][k] = f32x4{Y[4 * k], Y[4 * k + 1], Y[4 * k + 2], Y[4 * k + 3]};
+#pragma unroll
+    for (int q = 0; q < kMaxRadial / 4; ++q)
+      if (q < nq)
+        sPhi[threadIdx.x][q] = f32x4{radial_phi(len, 4 * q, sigma), radial_phi(len, 4 * q + 1, sigma),
+                                     radial_phi(len, 4 * q + 2, sigma), radial_phi(len, 4 * q + 3, sigma)};
   }
   __syncthreads();
   if (r >= R) return;
+#pragma unroll 2
   for (int e = 0; e < n; ++e) {
     float v = 0.f, rho = 0.f;
 #pragma unroll
-    for (int k = 0; k < d; ++k) v = fmaf(sY[e][k], b[k], v);
+    for (int k = 0; k < dq; ++k) {
+      const f32x4 y = sY[e][k];
 #pragma unroll
-    for (int q = 0; q < kMaxRadial; ++q) rho = fmaf(sPhi[e][q], w[q], rho);
+      for (int i = 0; i < 4; ++i) v = fmaf(y[i], b[k][i], v);
+    }
+#pragma unroll
+    for (int q = 0; q < kMaxRadial / 4; ++q)
+      if (q < nq) {
+        const f32x4 p = sPhi[e][q];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rho = fmaf(p[i], w[q][i], rho);
+      }
     g[size_t(e0 + e) * R + r] = v * rho;
   }
 }
 
-// ---- dg_e and, per rank tile, its share of dalpha_e
+// ---- dg_e and dalpha_e
 struct DgArgs {
   int E, C, R, RT, H, n_range;
   const int32_t *perm, *src, *dst;
-  const uint32_t *xp, *gp;        // x and Gz in launch_feature_layout_packed's words
+  const u32x4 *xp, *gp;            // x and Gz in launch_feature_layout_packed's words
   const float *x_scale, *g_scale;  // their row scales
-  const u32x4* ops;               // k_att_factors
+  const u32x4* ops;                // k_att_factors
   const float* f_scale;
-  const float* g;                 // [E, R] by sorted position
-  const float* alpha;             // [E, H] by sorted position
-  float* dg;                      // [E, R]
-  float* dal;                     // [RT, E, H]
+  const float* g;                  // [E, R] by sorted position
+  const float* alpha;              // [E, H] by sorted position
+  float* dg;                       // [E, R]
+  float* dal;                      // [E, H]
 };
 
 template <int CTRL>
@@ -132,44 +147,90 @@ __device__ __forceinline__ float half_sum(float v) {
   v = dpp_add<0x4E>(v);   // quad_perm [2, 3, 0, 1]
   v = dpp_add<0x141>(v);  // mirrored within 8 lanes
   v = dpp_add<0x140>(v);  // mirrored within 16 lanes
-  return v + __shfl_xor(v, 16);
+  const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
 }
-__device__ __forceinline__ float both_halves(float v) {
-  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+// lanes 0 .. 31: the sum of a over the lane and its other half; lanes 32 .. 63: of b
+__device__ __forceinline__ float halves_of_two(float a, float b) {
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+__device__ __forceinline__ float both_halves(float v) { return halves_of_two(v, v); }
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
-// A wave takes one range of sorted edges and one tile of 32 ranks; the waves
-// of a workgroup share a range as far as there are tiles, so that a source's
-// words are read once from L2.
+// A workgroup takes one range of sorted edges, a wave one tile of 32 ranks.
+// The range is a stream of items, x[s_e] of every edge and, before the first
+// edge of each destination, Gz[t]: one node's packed words each, brought into
+// one of two LDS slots by direct loads while the item before is worked on, so
+// that each item is read from L2 once for all ranks.  Bound by the matrix
+// instructions and, beside them, the sums of U V.
 template <int L, int CT>
-__global__ __launch_bounds__(256) void k_att_dg(DgArgs a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_att_dg(DgArgs a) {
   constexpr int d = (L + 1) * (L + 1), n = pk_rows(d), nb = pk_blocks(d), n4 = n / 4, nt = n % 4;
-  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int item = xcd_remap(blockIdx.x, gridDim.x) * 4 + wave;
-  const int range = item / a.RT, rt = item - range * a.RT;
-  if (range >= a.n_range) return;
+  extern __shared__ u32x4 smem[];  // two slots of a node's words, then [RT][64][H] of dalpha's shares
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int rt = __builtin_amdgcn_readfirstlane(tid >> 6);  // the wave's rank tile
+  const int RT = a.RT, H = a.H, R = a.R, threads = RT * kWave;
+  const int range = xcd_remap(blockIdx.x, gridDim.x);
   const int e0 = int(int64_t(range) * a.E / a.n_range), e1 = int(int64_t(range + 1) * a.E / a.n_range);
-  if (e0 >= e1) return;
-  const int ct_n = a.C / kTile, per_head = ct_n / a.H, H = a.H, R = a.R;
+  if (e0 >= e1) return;  // (the whole workgroup)
+  const int ct_n = a.C / kTile, per_head = ct_n / H;
+  const int words4 = ct_n * 16 * n;  // a node's words, sixteen bytes each
+  float* s_dal = reinterpret_cast<float*>(smem + 2 * words4);
   const int r = rt * kTile + l32;
-  const float un = a.f_scale[r] * a.f_scale[a.RT * kTile + r];
+  const float un = a.f_scale[r] * a.f_scale[RT * kTile + r];
   u32x4 Aop[nb];
 #pragma unroll
-  for (int b = 0; b < nb; ++b) Aop[b] = a.ops[(size_t(b) * a.RT + rt) * kWave + lane];
-  const u32x4* Dop = a.ops + size_t(nb) * a.RT * kWave;
-  // a node's words of one channel tile, as the K blocks of the contraction
-  auto load_words = [&](const uint32_t* base, int node, int ct, uint32_t (&w)[n]) {
-    const uint32_t* p = base + (size_t(node) * ct_n + ct) * 64 * n;
+  for (int b = 0; b < nb; ++b) Aop[b] = a.ops[(size_t(b) * RT + rt) * kWave + lane];
+  const u32x4* Dop = a.ops + (size_t(nb) * RT + rt) * kWave + lane;
+  // records of 64 sorted edges, one a lane, and of the 64 after them
+  struct Rec {
+    int src, dst;
+    float sc, al[kMaxH];
+  };
+  auto load_batch = [&](int b0) {
+    Rec rec{0, -1, 1.f, {}};
+    if (b0 + lane < e1) {
+      const int eid = a.perm[b0 + lane];
+      rec.src = a.src[eid];
+      rec.dst = a.dst[eid];
+      rec.sc = a.x_scale[rec.src] * a.g_scale[rec.dst];
+#pragma unroll
+      for (int k = 0; k < kMaxH; ++k)
+        if (k < H) rec.al[k] = a.alpha[size_t(b0 + lane) * H + k];
+    }
+    return rec;
+  };
+  Rec cur = load_batch(e0), nxt = load_batch(e0 + kWave);
+  int b0 = e0;
+  auto of = [&](int in_cur, int in_nxt, int e) {
+    const int i = e - b0;
+    return i < kWave ? __builtin_amdgcn_readlane(in_cur, i) : __builtin_amdgcn_readlane(in_nxt, i - kWave);
+  };
+  auto src_of = [&](int e) { return of(cur.src, nxt.src, e); };
+  auto dst_of = [&](int e) { return of(cur.dst, nxt.dst, e); };
+  auto fetch = [&](const u32x4* base, int node, int slot) {
+    const u32x4* src = base + size_t(node) * words4;
+    u32x4* dst = smem + slot * words4;
+    for (int i = rt * kWave; i < words4; i += threads)
+      if (i + lane < words4)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + i + lane),
+                                         (__attribute__((address_space(3))) void*)(dst + i), 16, 0, 0);
+  };
+  // channel tile ct of the item in a slot, as the K blocks of a contraction
+  auto load_words = [&](const u32x4* slot, int ct, uint32_t (&w)[n]) {
+    const u32x4* p = slot + ct * 16 * n;
 #pragma unroll
     for (int q = 0; q < n4; ++q) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(p + q * 256 + 4 * lane);
+      const u32x4 v = p[q * kWave + lane];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[4 * q + i] = v[i];
     }
+    const uint32_t* t = reinterpret_cast<const uint32_t*>(p + n4 * kWave) + nt * lane;
 #pragma unroll
-    for (int i = 0; i < nt; ++i) w[4 * n4 + i] = p[n4 * 256 + nt * lane + i];
+    for (int i = 0; i < nt; ++i) w[4 * n4 + i] = t[i];
   };
   auto block = [&](const uint32_t (&w)[n], int b) {
     u32x4 v;
@@ -177,77 +238,91 @@ __global__ __launch_bounds__(256) void k_att_dg(DgArgs a) {
     for (int k = 0; k < 4; ++k) v[k] = w[4 * b + k < n ? 4 * b + k : 4 * b + k - n];
     return v;
   };
-  struct Rec {
-    int src, dst;
-    float sc;
+  auto item_ready = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share is in LDS
+    __syncthreads();                     // every wave's is, and the other slot is free
   };
-  auto load_batch = [&](int b0) {
-    Rec rec{0, -1, 1.f};
-    if (b0 + lane < e1) {
-      const int eid = a.perm[b0 + lane];
-      rec.src = a.src[eid];
-      rec.dst = a.dst[eid];
-      rec.sc = a.x_scale[rec.src] * a.g_scale[rec.dst];
-    }
-    return rec;
-  };
-  Rec cur = load_batch(e0), nxt = load_batch(e0 + kWave);
-  int b0 = e0, t_cur = -1;
   f32x16 U[CT];
-  uint32_t xw[n];
-  load_words(a.xp, __builtin_amdgcn_readlane(cur.src, 0), 0, xw);
+  fetch(a.gp, dst_of(e0), 0);
+  int slot = 0, t_cur = -1;
+  float g_next = r < R ? a.g[size_t(e0) * R + r] : 0.f;
   for (int e = e0; e < e1; ++e) {
     const int j = e - b0;
-    const int s = __builtin_amdgcn_readlane(cur.src, j), t = __builtin_amdgcn_readlane(cur.dst, j);
-    const float sc = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, cur.sc), j)) * un;
-    const int s_next = e + 1 >= e1 ? s
-                                   : (j + 1 < kWave ? __builtin_amdgcn_readlane(cur.src, j + 1)
-                                                    : __builtin_amdgcn_readlane(nxt.src, 0));
-    if (t != t_cur) {
+    const int t = __builtin_amdgcn_readlane(cur.dst, j);
+    if (t != t_cur) {  // Gz[t] is in the slot: U_t, while x[s_e] comes
       t_cur = t;
+      item_ready();
+      fetch(a.xp, __builtin_amdgcn_readlane(cur.src, j), slot ^ 1);
+      u32x4 Dv[nb];
+#pragma unroll
+      for (int b = 0; b < nb; ++b) Dv[b] = Dop[size_t(b) * RT * kWave];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
         if (ct < ct_n) {
           uint32_t w[n];
-          load_words(a.gp, t, ct, w);
+          load_words(smem + slot * words4, ct, w);
           f32x16 acc = f32x16{};
 #pragma unroll
-          for (int b = 0; b < nb; ++b) acc = mfma_f16(block(w, b), Dop[(size_t(b) * a.RT + rt) * kWave + lane], acc);
+          for (int b = 0; b < nb; ++b) acc = mfma_f16(block(w, b), Dv[b], acc);
           U[ct] = acc;
         }
+      slot ^= 1;
     }
-    const float ge = r < R ? a.g[size_t(e) * R + r] : 0.f;
+    item_ready();
+    const float ge = g_next;
+    if (e + 1 < e1) {
+      const int tn = dst_of(e + 1);
+      fetch(tn != t ? a.gp : a.xp, tn != t ? tn : src_of(e + 1), slot ^ 1);
+      g_next = r < R ? a.g[size_t(e + 1) * R + r] : 0.f;
+    }
     float p[CT];
+    uint32_t w[2][n];
+    load_words(smem + slot * words4, 0, w[0]);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       p[ct] = 0.f;
       if (ct < ct_n) {
-        uint32_t nw[n];
-        const bool last = ct + 1 == ct_n;
-        load_words(a.xp, last ? s_next : s, last ? 0 : ct + 1, nw);
+        if (ct + 1 < CT) load_words(smem + slot * words4, min(ct + 1, ct_n - 1), w[(ct + 1) & 1]);
         f32x16 V = f32x16{};
 #pragma unroll
-        for (int b = 0; b < nb; ++b) V = mfma_f16(block(xw, b), Aop[b], V);
+        for (int b = 0; b < nb; ++b) V = mfma_f16(block(w[ct & 1], b), Aop[b], V);
+        float q[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int v = 0; v < 16; ++v) p[ct] = fmaf(U[ct][v], V[v], p[ct]);
-#pragma unroll
-        for (int i = 0; i < n; ++i) xw[i] = nw[i];
+        for (int v = 0; v < 16; ++v) q[v & 3] = fmaf(U[ct][v], V[v], q[v & 3]);
+        p[ct] = (q[0] + q[1]) + (q[2] + q[3]);
       }
     }
-    // per head: this lane's half of the channels, then both
+    slot ^= 1;
+    // heads in pairs: one's sums over channels in lanes 0 .. 31, the other's
+    // in lanes 32 .. 63
+    const float sc = lane_value(cur.sc, j) * un;
     float dge = 0.f;
-    for (int k = 0; k < H; ++k) {
-      float P = 0.f;
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-        if (ct / per_head == k) P += p[ct];
-      P = both_halves(P) * sc;
-      dge = fmaf(a.alpha[size_t(e) * H + k], P, dge);
-      const float da = half_sum(P * ge);
-      if (lane == 0) a.dal[(size_t(rt) * a.E + e) * H + k] = da;
-    }
+    for (int k = 0; k < kMaxH; k += 2)
+      if (k < H) {
+        float P0 = 0.f, P1 = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          if (ct / per_head == k) P0 += p[ct];
+          if (ct / per_head == k + 1) P1 += p[ct];
+        }
+        const float P = halves_of_two(P0, P1) * sc;
+        const float al0 = lane_value(cur.al[k], j), al1 = k + 1 < H ? lane_value(cur.al[k + 1], j) : 0.f;
+        dge = fmaf(h ? al1 : al0, P, dge);
+        const float da = half_sum(P * ge);
+        if (l32 == 0 && k + h < H) s_dal[(rt * kWave + j) * H + k + h] = da;
+      }
+    dge = both_halves(dge);
     if (h == 0 && r < R) a.dg[size_t(e) * R + r] = dge;
-    if (j + 1 == kWave) {
+    if (j + 1 == kWave || e + 1 == e1) {
+      // dalpha of the batch: the rank tiles' shares in order
+      __syncthreads();
+      for (int i = tid; i < (j + 1) * H; i += threads) {
+        float v = 0.f;
+        for (int q = 0; q < RT; ++q) v += s_dal[q * kWave * H + i];
+        a.dal[size_t(b0) * H + i] = v;
+      }
+      __syncthreads();
       cur = nxt;
       b0 += kWave;
       nxt = load_batch(b0 + kWave);
@@ -260,7 +335,7 @@ __global__ __launch_bounds__(256) void k_att_dg(DgArgs a) {
 // [gridDim.x][n_radial + H][F].
 constexpr int kDaWaves = 4;
 __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
-    int N, int E, int C, int F, int H, int nr, int RT, float sigma, const int32_t* __restrict__ offsets,
+    int N, int C, int F, int H, int nr, float sigma, const int32_t* __restrict__ offsets,
     const int32_t* __restrict__ perm, const int32_t* __restrict__ src, const float* __restrict__ edge_vec,
     const float* __restrict__ Pt, const float* __restrict__ Ps, const float* __restrict__ W1,
     const float* __restrict__ w2, const float* __restrict__ alpha, const float* __restrict__ dal,
@@ -285,12 +360,7 @@ __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
     wo[k] = unit && k < H ? w2[lane * H + k] : 0.f;
     go[k] = 0.f;
   }
-  // dalpha of sorted edge e and head k: the rank tiles' shares in order
-  auto dalpha = [&](int e, int k) {
-    float v = 0.f;
-    for (int rt = 0; rt < RT; ++rt) v += dal[(size_t(rt) * E + e) * H + k];
-    return v;
-  };
+  auto dalpha = [&](int e, int k) { return dal[size_t(e) * H + k]; };
   for (int t = blockIdx.x * kDaWaves + wv; t < N; t += gridDim.x * kDaWaves) {
     const int e0 = offsets[t], e1 = offsets[t + 1];
     float dpt = 0.f;
@@ -399,10 +469,22 @@ __global__ __launch_bounds__(256) void k_att_dps(int N, int F, int H, const int3
   for (int i = e0 * H + lane; i < e1 * H; i += kWave)
     alpha_src[i] = alpha_eid[size_t(perm[i / H]) * H + i % H];
   float v = 0.f;
-  if (lane < F) {
-    for (int e = e0; e < e1; ++e) v += dhid[size_t(perm[e]) * F + lane];
-    dPs[size_t(s) * F + lane] = v;
+  const bool unit = lane < F;
+  for (int b = e0; b < e1; b += kWave) {
+    const int cnt = min(kWave, e1 - b), eid = lane < cnt ? perm[b + lane] : 0;
+    // eight rows in flight, added in order
+    for (int i = 0; i < cnt; i += 8) {
+      float r[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int id = __builtin_amdgcn_readlane(eid, min(i + k, cnt - 1));
+        r[k] = unit && i + k < cnt ? dhid[size_t(id) * F + lane] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += r[k];
+    }
   }
+  if (unit) dPs[size_t(s) * F + lane] = v;
 }
 
 // ---- grad_x of the degree-0 rows: += dPt[n] W1[0 .. C)^T + dPs[n] W1[C .. 2C)^T;
@@ -464,15 +546,20 @@ __global__ __launch_bounds__(256) void k_att_dw1(int N, int d, int C, int F, con
     partial[(size_t(blockIdx.y) * 2 * C + which * C + ct * kTile + acc_row(v, h)) * F + f] = acc[v];
 }
 
+// LDS of k_att_dg: two nodes' words and dalpha's shares of a batch
+int dg_lds(const AttBwdArgs& a) {
+  const int RT = (a.R + kTile - 1) / kTile;
+  return 2 * (a.C / kTile) * 256 * pk_rows(a.d) + RT * kWave * a.H * 4;
+}
+
 template <int L>
 hipError_t launch_dg_l(const AttBwdArgs& a, const DgArgs& g, hipStream_t s) {
-  const int blocks = (g.n_range * g.RT + 3) / 4, ct = a.C / kTile;
-  if (ct <= 2)
-    k_att_dg<L, 2><<<dim3(blocks), dim3(256), 0, s>>>(g);
-  else if (ct <= 4)
-    k_att_dg<L, 4><<<dim3(blocks), dim3(256), 0, s>>>(g);
-  else
-    k_att_dg<L, 8><<<dim3(blocks), dim3(256), 0, s>>>(g);
+  const int ct = a.C / kTile, lds = dg_lds(a);
+  auto k = ct <= 2 ? k_att_dg<L, 2> : (ct <= 4 ? k_att_dg<L, 4> : k_att_dg<L, 8>);
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  k<<<dim3(g.n_range), dim3(g.RT * kWave), lds, s>>>(g);
   return hipGetLastError();
 }
 template <int L>
@@ -522,14 +609,15 @@ hipError_t launch_att_bwd_dg(const AttBwdArgs& a, hipStream_t s) {
   g.R = a.R;
   g.RT = RT;
   g.H = a.H;
-  // two waves a SIMD up to 128 channels, one above (registers)
-  const int waves = device_cus() * (ct <= 4 ? 8 : 4), ranges = waves / RT;
-  g.n_range = ranges < 1 ? 1 : (ranges < a.E ? ranges : a.E);
+  // as many workgroups as the device holds at two waves a SIMD
+  const int by_lds = 160 * 1024 / dg_lds(a), by_waves = 8 / RT, per_cu = by_lds < by_waves ? by_lds : by_waves;
+  const int ranges = device_cus() * (per_cu < 1 ? 1 : per_cu);
+  g.n_range = ranges < a.E ? ranges : a.E;
   g.perm = a.perm;
   g.src = a.src;
   g.dst = a.dst;
-  g.xp = static_cast<const uint32_t*>(a.xp);
-  g.gp = static_cast<const uint32_t*>(a.gp);
+  g.xp = static_cast<const u32x4*>(a.xp);
+  g.gp = static_cast<const u32x4*>(a.gp);
   g.x_scale = a.x_scale;
   g.g_scale = a.g_scale;
   g.ops = ops;
@@ -552,7 +640,7 @@ hipError_t launch_att_bwd_mlp(const AttBwdArgs& a, hipStream_t s) {
     return hipErrorInvalidValue;
   const int nb = att_bwd_da_blocks(a.N), rows = a.n_radial + a.H;
   k_att_da<<<dim3(nb), dim3(kDaWaves * kWave), 0, s>>>(
-      a.N, a.E, a.C, a.F, a.H, a.n_radial, (a.R + kTile - 1) / kTile, a.sigma, a.offsets, a.perm, a.src, a.edge_vec,
+      a.N, a.C, a.F, a.H, a.n_radial, a.sigma, a.offsets, a.perm, a.src, a.edge_vec,
       a.Pt, a.Ps, a.W1, a.w2, a.alpha, a.dal, a.dhid, a.dPt, a.grad_vec, a.part_da);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

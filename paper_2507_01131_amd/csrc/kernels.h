@@ -163,8 +163,8 @@ hipError_t launch_att_alpha(int N, int C, int F, int H, int n_radial, float sigm
                             const float* Ps, const float* W1, const float* w2, float* alpha_sorted,
                             float* alpha_eid, hipStream_t s);
 // The block's backward (attention_bwd.hip; 1 <= L <= 4, R <= 256, fp32).
-// launch_att_bwd_dg: dg [E, R] by sorted position and the rank tiles' shares
-// dal [ceil(R / 32), E, H] of dalpha, from x and Gz in the packed layout.
+// launch_att_bwd_dg: dg [E, R] and dalpha dal [E, H] by sorted position, from x
+// and Gz in the packed layout.
 // launch_att_bwd_mlp: the softmax and the logits' MLP; adds to grad_vec (if
 // not nullptr), and writes dhid, dPt, dPs, alpha_src, grad_w1 and grad_w2 (the
 // last two may be nullptr).  launch_att_bwd_x0: adds what the logits owe to
@@ -182,7 +182,7 @@ struct AttBwdArgs {
   const float *Pt, *Ps;                   // launch_att_node
   const float *alpha, *alpha_eid;         // [E, H] by sorted position, by edge id
   float* alpha_src;                       // [E, H] in the order of perm_src
-  float *g, *dg, *dal;                    // [E, R], [E, R], [ceil(R / 32), E, H]
+  float *g, *dg, *dal;                    // [E, R], [E, R], [E, H]
   float *dhid, *dPt, *dPs;                // [E, F] by edge id, [N, F], [N, F]
   float *part_da, *sum_da;                // [att_bwd_da_blocks(N)][n_radial + H][F], [n_radial + H][F]
   float* part_w1;                         // [att_bwd_dw1_parts(N)][2 C][F]
