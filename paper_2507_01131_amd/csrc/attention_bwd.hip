@@ -30,6 +30,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMaxF = 64, kMaxH = 8, kMaxRadial = 16;
 constexpr float kLeaky = 0.2f;
+constexpr int kBufferWord3 = 0x00020000;  // raw buffer resource, fourth word (gfx9 family)
 
 __device__ __forceinline__ f32x16 mfma_f16(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
@@ -160,6 +161,12 @@ __device__ __forceinline__ float lane_value(float v, int lane) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
+// waves a SIMD that the registers allow
+__host__ __device__ constexpr int dg_waves(int CT) { return CT <= 2 ? 3 : 2; }
+
+// sixteen-byte words of a slot: a node's, in whole direct loads of a wave
+__host__ __device__ constexpr int dg_slot(int ct_n, int n) { return (ct_n * 16 * n + kWave - 1) / kWave * kWave; }
+
 // A workgroup takes one range of sorted edges, a wave one tile of 32 ranks.
 // The range is a stream of items, x[s_e] of every edge and, before the first
 // edge of each destination, Gz[t]: one node's packed words each, brought into
@@ -167,9 +174,9 @@ __device__ __forceinline__ float lane_value(float v, int lane) {
 // that each item is read from L2 once for all ranks.  Bound by the matrix
 // instructions and, beside them, the sums of U V.
 template <int L, int CT>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_att_dg(DgArgs a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(dg_waves(CT)))) void k_att_dg(DgArgs a) {
   constexpr int d = (L + 1) * (L + 1), n = pk_rows(d), nb = pk_blocks(d), n4 = n / 4, nt = n % 4;
-  extern __shared__ u32x4 smem[];  // two slots of a node's words, then [RT][64][H] of dalpha's shares
+  extern __shared__ u32x4 smem[];  // two slots of a node's words, [RT][64][H] of dalpha's shares, alpha
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int rt = __builtin_amdgcn_readfirstlane(tid >> 6);  // the wave's rank tile
   const int RT = a.RT, H = a.H, R = a.R, threads = RT * kWave;
@@ -177,8 +184,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int e0 = int(int64_t(range) * a.E / a.n_range), e1 = int(int64_t(range + 1) * a.E / a.n_range);
   if (e0 >= e1) return;  // (the whole workgroup)
   const int ct_n = a.C / kTile, per_head = ct_n / H;
-  const int words4 = ct_n * 16 * n;  // a node's words, sixteen bytes each
-  float* s_dal = reinterpret_cast<float*>(smem + 2 * words4);
+  const int words4 = ct_n * 16 * n, slot4 = dg_slot(ct_n, n);  // a node's words, sixteen bytes each
+  float* s_dal = reinterpret_cast<float*>(smem + 2 * slot4);
+  float* s_al = s_dal + RT * kWave * H;  // alpha of the batch [64][H]
   const int r = rt * kTile + l32;
   const float un = a.f_scale[r] * a.f_scale[RT * kTile + r];
   u32x4 Aop[nb];
@@ -188,20 +196,20 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   // records of 64 sorted edges, one a lane, and of the 64 after them
   struct Rec {
     int src, dst;
-    float sc, al[kMaxH];
+    float sc;
   };
   auto load_batch = [&](int b0) {
-    Rec rec{0, -1, 1.f, {}};
+    Rec rec{0, -1, 1.f};
     if (b0 + lane < e1) {
       const int eid = a.perm[b0 + lane];
       rec.src = a.src[eid];
       rec.dst = a.dst[eid];
       rec.sc = a.x_scale[rec.src] * a.g_scale[rec.dst];
-#pragma unroll
-      for (int k = 0; k < kMaxH; ++k)
-        if (k < H) rec.al[k] = a.alpha[size_t(b0 + lane) * H + k];
     }
     return rec;
+  };
+  auto load_alpha = [&](int b0) {
+    for (int i = tid; i < min(kWave, e1 - b0) * H; i += threads) s_al[i] = a.alpha[size_t(b0) * H + i];
   };
   Rec cur = load_batch(e0), nxt = load_batch(e0 + kWave);
   int b0 = e0;
@@ -211,13 +219,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   };
   auto src_of = [&](int e) { return of(cur.src, nxt.src, e); };
   auto dst_of = [&](int e) { return of(cur.dst, nxt.dst, e); };
+  // (lanes behind the node's words read zeros through the range check, into
+  // the slot's padding)
   auto fetch = [&](const u32x4* base, int node, int slot) {
-    const u32x4* src = base + size_t(node) * words4;
-    u32x4* dst = smem + slot * words4;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<u32x4*>(base) + size_t(node) * words4, 0, words4 * 16, kBufferWord3);
+    u32x4* dst = smem + slot * slot4;
     for (int i = rt * kWave; i < words4; i += threads)
-      if (i + lane < words4)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + i + lane),
-                                         (__attribute__((address_space(3))) void*)(dst + i), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(dst + i), 16, lane * 16,
+                                               i * 16, 0, 0);
   };
   // channel tile ct of the item in a slot, as the K blocks of a contraction
   auto load_words = [&](const u32x4* slot, int ct, uint32_t (&w)[n]) {
@@ -243,6 +253,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     __syncthreads();                     // every wave's is, and the other slot is free
   };
   f32x16 U[CT];
+  load_alpha(e0);  // (read behind the next barrier)
   fetch(a.gp, dst_of(e0), 0);
   int slot = 0, t_cur = -1;
   float g_next = r < R ? a.g[size_t(e0) * R + r] : 0.f;
@@ -260,7 +271,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       for (int ct = 0; ct < CT; ++ct)
         if (ct < ct_n) {
           uint32_t w[n];
-          load_words(smem + slot * words4, ct, w);
+          load_words(smem + slot * slot4, ct, w);
           f32x16 acc = f32x16{};
 #pragma unroll
           for (int b = 0; b < nb; ++b) acc = mfma_f16(block(w, b), Dv[b], acc);
@@ -275,43 +286,46 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       fetch(tn != t ? a.gp : a.xp, tn != t ? tn : src_of(e + 1), slot ^ 1);
       g_next = r < R ? a.g[size_t(e + 1) * R + r] : 0.f;
     }
-    float p[CT];
+    const float sc = lane_value(cur.sc, j) * un;
+    // heads in pairs: one's sums over channels in lanes 0 .. 31, the other's
+    // in lanes 32 .. 63
+    float dge = 0.f, first = 0.f, sum = 0.f;
+    int k = 0, left = per_head;
+    auto pair_done = [&](float P0, float P1, int k0) {
+      const int kh = min(k0 + h, H - 1);
+      const float al = k0 + h < H ? s_al[j * H + kh] : 0.f;
+      const float P = halves_of_two(P0, P1) * sc;
+      dge = fmaf(al, P, dge);
+      const float da = half_sum(P * ge);
+      if (l32 == 0 && k0 + h < H) s_dal[(rt * kWave + j) * H + kh] = da;
+    };
     uint32_t w[2][n];
-    load_words(smem + slot * words4, 0, w[0]);
+    load_words(smem + slot * slot4, 0, w[0]);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      p[ct] = 0.f;
       if (ct < ct_n) {
-        if (ct + 1 < CT) load_words(smem + slot * words4, min(ct + 1, ct_n - 1), w[(ct + 1) & 1]);
+        if (ct + 1 < CT) load_words(smem + slot * slot4, min(ct + 1, ct_n - 1), w[(ct + 1) & 1]);
         f32x16 V = f32x16{};
 #pragma unroll
         for (int b = 0; b < nb; ++b) V = mfma_f16(block(w[ct & 1], b), Aop[b], V);
         float q[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < 16; ++v) q[v & 3] = fmaf(U[ct][v], V[v], q[v & 3]);
-        p[ct] = (q[0] + q[1]) + (q[2] + q[3]);
+        sum += (q[0] + q[1]) + (q[2] + q[3]);
+        if (--left == 0) {
+          left = per_head;
+          if (k & 1)
+            pair_done(first, sum, k - 1);
+          else if (k + 1 == H)
+            pair_done(sum, 0.f, k);
+          else
+            first = sum;
+          sum = 0.f;
+          ++k;
+        }
       }
     }
     slot ^= 1;
-    // heads in pairs: one's sums over channels in lanes 0 .. 31, the other's
-    // in lanes 32 .. 63
-    const float sc = lane_value(cur.sc, j) * un;
-    float dge = 0.f;
-#pragma unroll
-    for (int k = 0; k < kMaxH; k += 2)
-      if (k < H) {
-        float P0 = 0.f, P1 = 0.f;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          if (ct / per_head == k) P0 += p[ct];
-          if (ct / per_head == k + 1) P1 += p[ct];
-        }
-        const float P = halves_of_two(P0, P1) * sc;
-        const float al0 = lane_value(cur.al[k], j), al1 = k + 1 < H ? lane_value(cur.al[k + 1], j) : 0.f;
-        dge = fmaf(h ? al1 : al0, P, dge);
-        const float da = half_sum(P * ge);
-        if (l32 == 0 && k + h < H) s_dal[(rt * kWave + j) * H + k + h] = da;
-      }
     dge = both_halves(dge);
     if (h == 0 && r < R) a.dg[size_t(e) * R + r] = dge;
     if (j + 1 == kWave || e + 1 == e1) {
@@ -326,6 +340,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       cur = nxt;
       b0 += kWave;
       nxt = load_batch(b0 + kWave);
+      load_alpha(b0);
     }
   }
 }
@@ -546,10 +561,10 @@ __global__ __launch_bounds__(256) void k_att_dw1(int N, int d, int C, int F, con
     partial[(size_t(blockIdx.y) * 2 * C + which * C + ct * kTile + acc_row(v, h)) * F + f] = acc[v];
 }
 
-// LDS of k_att_dg: two nodes' words and dalpha's shares of a batch
+// LDS of k_att_dg: two nodes' words, then a batch's shares of dalpha and its alpha
 int dg_lds(const AttBwdArgs& a) {
   const int RT = (a.R + kTile - 1) / kTile;
-  return 2 * (a.C / kTile) * 256 * pk_rows(a.d) + RT * kWave * a.H * 4;
+  return 2 * 16 * dg_slot(a.C / kTile, pk_rows(a.d)) + (RT + 1) * kWave * a.H * 4;
 }
 
 template <int L>
@@ -609,8 +624,8 @@ hipError_t launch_att_bwd_dg(const AttBwdArgs& a, hipStream_t s) {
   g.R = a.R;
   g.RT = RT;
   g.H = a.H;
-  // as many workgroups as the device holds at two waves a SIMD
-  const int by_lds = 160 * 1024 / dg_lds(a), by_waves = 8 / RT, per_cu = by_lds < by_waves ? by_lds : by_waves;
+  // as many workgroups as the device holds
+  const int by_lds = 160 * 1024 / dg_lds(a), by_waves = 4 * dg_waves(ct) / RT, per_cu = by_lds < by_waves ? by_lds : by_waves;
   const int ranges = device_cus() * (per_cu < 1 ? 1 : per_cu);
   g.n_range = ranges < a.E ? ranges : a.E;
   g.perm = a.perm;

@@ -530,8 +530,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
 // A workgroup takes 128 nodes; the packed weights go through LDS as in
 // k_ffn_rows.
 template <int CT, bool BF>
-__global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const float* __restrict__ dq,
-                                                 const u32x4* __restrict__ wg, const int* __restrict__ eg,
+__global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const float* __restrict__ sum,
+                                                 const float* __restrict__ slope, const u32x4* __restrict__ wg, const int* __restrict__ eg,
                                                  float* __restrict__ r0) {
   constexpr int P = BF ? 1 : 2, kHalf = 2 * CT * P * kBlk;
   extern __shared__ u32x4 sw[];  // [2][kHalf]
@@ -539,7 +539,8 @@ __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const flo
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = (blockIdx.x * 4 + wave) * kTile + l32;
   const int f0 = blockIdx.y * FT / gridDim.y, f1 = (blockIdx.y + 1) * FT / gridDim.y;
-  const float* q = dq + size_t(min(n, N - 1)) * 32 * FT + 4 * h;
+  const float* q = sum + size_t(min(n, N - 1)) * 32 * FT + 4 * h;
+  const float* ds = slope + size_t(min(n, N - 1)) * 32 * FT + 4 * h;
   auto fetch = [&](int ft, int buf) {
     const u32x4* src = wg + size_t(ft) * kHalf;
     u32x4* dst = sw + buf * kHalf;
@@ -548,9 +549,15 @@ __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const flo
       if (wave < 2) blocks_to_lds<1>(src + 4 * (CT * P / 2) * kBlk, dst + 4 * (CT * P / 2) * kBlk, wave, lane);
   };
   fetch(f0, 0);
-  f32x4 dv[4];
+  f32x4 dv[4], sv[4];
+  auto load = [&](int ft) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) dv[k] = *reinterpret_cast<const f32x4*>(q + 32 * f0 + 8 * k);
+    for (int k = 0; k < 4; ++k) {
+      dv[k] = *reinterpret_cast<const f32x4*>(q + 32 * ft + 8 * k);
+      sv[k] = *reinterpret_cast<const f32x4*>(ds + 32 * ft + 8 * k);
+    }
+  };
+  load(f0);
   f32x16 acc[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x16{};
@@ -560,10 +567,8 @@ __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const flo
     if (ft + 1 < f1) fetch(ft + 1, (ft + 1 - f0) & 1);
     float t[16];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) t[v] = dv[v >> 2][v & 3];
-    if (ft + 1 < f1)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) dv[k] = *reinterpret_cast<const f32x4*>(q + 32 * (ft + 1) + 8 * k);
+    for (int v = 0; v < 16; ++v) t[v] = dv[v >> 2][v & 3] * sv[v >> 2][v & 3];
+    if (ft + 1 < f1) load(ft + 1);
     u32x4 o[2][P];
     to_operand<BF>(t, BF ? 0 : eg[ft], E, o, [&](float f) {
 #pragma unroll
@@ -601,7 +606,8 @@ __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const flo
 // tile also sum dq (grad b).  partial [S][C + 1][32 FT]: the last row is grad b.
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, int FT, const void* __restrict__ x,
-                                                 const float* __restrict__ dq, float* __restrict__ partial) {
+                                                 const float* __restrict__ row_sum, const float* __restrict__ slope,
+                                                 float* __restrict__ partial) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, l32 = lane & 31;
   const int FP = (FT + 1) / 2, t = blockIdx.x * 4 + wave;
   if (t >= CT * FP) return;
@@ -611,7 +617,7 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
   f32x16 acc[2] = {f32x16{}, f32x16{}};
   float sum[2] = {0.f, 0.f};
   struct Step {
-    float b[2][8];
+    float b[2][8], c[2][8];  // the sum over rows and act'(q), whose product is dq
     float a[8];
     uint16_t ab[8];
   };
@@ -627,13 +633,21 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
       else
         s.a[k] = on && c < C ? static_cast<const float*>(x)[at * d * C + c] : 0.f;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) s.b[j][k] = on && (j == 0 || two) ? dq[at * Fp + 32 * (ft + j) + l32] : 0.f;
+      for (int j = 0; j < 2; ++j) {
+        const size_t i = at * Fp + 32 * (ft + j) + l32;
+        s.b[j][k] = on && (j == 0 || two) ? row_sum[i] : 0.f;
+        s.c[j][k] = on && (j == 0 || two) ? slope[i] : 0.f;
+      }
     }
   };
   Step cur, nxt;
   load(n0, cur);
   for (int n = n0; n < n1; n += 16) {
     if (n + 16 < n1) load(n + 16, nxt);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) cur.b[j][k] *= cur.c[j][k];
     if constexpr (BF) {
       u32x4 av;
 #pragma unroll
@@ -687,17 +701,24 @@ struct WgradArgs {
   const void *x, *gy;             // [N d, C]
   const u32x4 *up_u, *up_d;       // W_up and W_down^T packed as `up`
   const int *e_u, *e_d;
-  const float *s, *ds;            // act(q), act'(q) [N, 32 FT]
-  float* dq;                      // [N, 32 FT]
+  const float* s;                 // act(q) [N, 32 FT]
+  float* sum;                     // [N, 32 FT]: sum over a node's rows of dh u
   float* partial;                 // [gridDim.y][2][C][32 FT]: W_down's (as [c][f]), then W_up's
 };
 
 // Waves of a workgroup: two a SIMD where a wave's packed weights and sums leave
 // room in 256 registers.  A pair of waves has one tile of 32 hidden units.
 __host__ __device__ constexpr int wgrad_waves(int CT, bool BF) { return BF || CT <= 6 ? 8 : 4; }
+// Operand blocks that k_ffn_wgrad writes itself: each lane half 33 words apart
+// instead of 32, so that the 4 x 4 blocks' writes spread over the LDS banks;
+// and in the transposed order channel c of a tile at place wgrad_slot(c), so
+// that threads with neighbouring channels write neighbouring words.  Either
+// way a wave reads 32 words in some order.
+constexpr int kHalfW = 33, kBlkW = 2 * kHalfW;
+__device__ __forceinline__ int wgrad_slot(int c) { return (c & 3) * 8 + (c >> 2); }
 // LDS words: x and grad_y in both operand orders, then u and p of the pairs
 __host__ __device__ constexpr int wgrad_words(int CT, bool BF) {
-  return 4 * 2 * CT * (BF ? 1 : 2) * kBlk + wgrad_waves(CT, BF) * 4 * kBlk;
+  return 4 * 2 * CT * (BF ? 1 : 2) * kBlkW + wgrad_waves(CT, BF) * 4 * kBlk;
 }
 
 // four channels of a row as they lie in memory
@@ -715,7 +736,8 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     __attribute__((amdgpu_waves_per_eu(wgrad_waves(CT, BF) / 4, wgrad_waves(CT, BF) / 4))) void k_ffn_wgrad(
         WgradArgs a) {
   constexpr int P = BF ? 1 : 2, NT = wgrad_waves(CT, BF) * kWave;
-  constexpr int kOp = 2 * CT * P * kBlk;
+  constexpr int kOp = 2 * CT * P * kBlkW;  // words of a tensor in one operand order
+  constexpr int kPack = 2 * CT * P * kBlk;  // of a packed tile
   constexpr int kItems = (64 * CT + NT - 1) / NT;  // 4 x 4 blocks of a 32-row tile per thread and tensor
   extern __shared__ u32x4 smem[];
   __shared__ uint32_t s_max[2][32];
@@ -734,7 +756,7 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
   const bool own = tile < FT;
   u32x4 w[2 * CT][P];
   {
-    const u32x4* src = (role == 0 ? a.up_u : a.up_d) + size_t(ft) * kOp + lane;
+    const u32x4* src = (role == 0 ? a.up_u : a.up_d) + size_t(ft) * kPack + lane;
 #pragma unroll
     for (int st = 0; st < 2 * CT; ++st)
 #pragma unroll
@@ -742,8 +764,9 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
   }
   const int e_own = BF ? 0 : (role == 0 ? a.e_u : a.e_d)[ft], e_both = BF ? 0 : a.e_u[ft] + a.e_d[ft];
   // LDS: x in row order, x in transposed order, then grad_y in both
-  const u32x4* rows_op = smem + (role == 0 ? 0 : 2) * kOp + lane;  // x for u, grad_y for dh
-  const u32x4* cols_op = smem + (role == 0 ? 3 : 1) * kOp + lane;  // grad_y for W_down, x for W_up
+  const u32x4* rows_op = smem + (role == 0 ? 0 : 2) * kOp + h * kHalfW + l32;  // x for u, grad_y for dh
+  // grad_y for W_down, x for W_up
+  const u32x4* cols_op = smem + (role == 0 ? 3 : 1) * kOp + h * kHalfW + wgrad_slot(l32);
   f32x16 acc[CT];
   int E = kUnset;
 #pragma unroll
@@ -767,7 +790,7 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
         if (q + r >= n) break;
         run += v[r];
         if (++in_node == d) {
-          if (sums) a.dq[size_t(node) * Fp + 32 * ft + l32] = run * a.ds[size_t(node) * Fp + 32 * ft + l32];
+          if (sums) a.sum[size_t(node) * Fp + 32 * ft + l32] = run;
           run = 0.f;
           in_node = 0;
           ++node;
@@ -813,15 +836,15 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     for (int p = 0; p < P; ++p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        reinterpret_cast<uint2*>(op + (st * P + p) * kBlk + hh * 32 + 4 * rg + r)[(c >> 2) & 1] =
+        reinterpret_cast<uint2*>(op + (st * P + p) * kBlkW + hh * kHalfW + 4 * rg + r)[(c >> 2) & 1] =
             uint2{hl[p][r][0], hl[p][r][1]};
 #pragma unroll
       for (int cc = 0; cc < 4; ++cc) {
         const int k = cc >> 1, sh = 16 * (cc & 1);
         const uint32_t lo = ((hl[p][0][k] >> sh) & 0xffffu) | ((hl[p][1][k] >> sh) << 16);
         const uint32_t hi = ((hl[p][2][k] >> sh) & 0xffffu) | ((hl[p][3][k] >> sh) << 16);
-        reinterpret_cast<uint2*>(op + kOp + ((2 * ct + q) * P + p) * kBlk + ht * 32 + ((c + cc) & 31))[it] =
-            uint2{lo, hi};
+        reinterpret_cast<uint2*>(op + kOp + ((2 * ct + q) * P + p) * kBlkW + ht * kHalfW +
+                                 wgrad_slot((c + cc) & 31))[it] = uint2{lo, hi};
       }
     }
   };
@@ -883,6 +906,15 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
       }
     }
     __syncthreads();
+    // the gate of this lane's hidden unit for its rows' nodes (loads
+    // end in order: before the next tile's)
+    float s[16];
+    const float* sp = a.s + size_t(nb) * Fp + 32 * ft + l32;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int o = min(acc_row(v, h), r1 - 1 - rb);
+      s[v] = sp[int((uint32_t(mb + o) * inv_d) >> 16) * Fp];
+    }
     if (rb + 32 < r1) fetch(rb + 32);
     if constexpr (!BF)
       if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
@@ -892,16 +924,8 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     for (int st = 0; st < 2 * CT; ++st) {
       u32x4 op[P];
 #pragma unroll
-      for (int p = 0; p < P; ++p) op[p] = rows_op[(st * P + p) * kBlk];
+      for (int p = 0; p < P; ++p) op[p] = rows_op[(st * P + p) * kBlkW];
       t = mm_parts<BF>(op, w[st], t);
-    }
-    // the gate of this lane's hidden unit for its rows' nodes
-    float s[16];
-    const float* sp = a.s + size_t(nb) * Fp + 32 * ft + l32;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int o = min(acc_row(v, h), r1 - 1 - rb);
-      s[v] = sp[int((uint32_t(mb + o) * inv_d) >> 16) * Fp];
     }
     if (role == 0) {
 #pragma unroll
@@ -943,7 +967,7 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
       for (int q = 0; q < 2; ++q) {
         u32x4 op[P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) op[p] = cols_op[((2 * ct + q) * P + p) * kBlk];
+        for (int p = 0; p < P; ++p) op[p] = cols_op[((2 * ct + q) * P + p) * kBlkW];
         acc[ct] = mm_parts<BF>(op, o[q], acc[ct]);
       }
   }
@@ -1007,7 +1031,7 @@ __global__ __launch_bounds__(256) void k_ffn_wsum(int C, int F, int FT, int S, i
 size_t al256(size_t b) { return (b + 255) & ~size_t(255); }
 
 struct Layout {
-  size_t pack[5], exps, s, ds, dq, r0, part, part_g, total;
+  size_t pack[5], exps, s, ds, sum, r0, part, part_g, total;
   int CT, FT, P, S, Sg, KS;
   size_t pack_bytes;
 };
@@ -1032,7 +1056,7 @@ Layout layout(const FfnShape& p, bool backward) {
   if (backward) {
     l.ds = o;
     o += gate;
-    l.dq = o;
+    l.sum = o;
     o += gate;
     l.r0 = o;
     // shares of F, so that there is a workgroup a CU
@@ -1147,7 +1171,9 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   if (e == hipSuccess) e = gate<CT, BF>(l, p, a.x, ws, 3, a.b_gate, true, s);
   if (e != hipSuccess) return e;
   const int* ex = reinterpret_cast<const int*>(ws + l.exps);
-  float* dq = reinterpret_cast<float*>(ws + l.dq);
+  // dq = act'(q) sum, formed where it is read
+  float* sum = reinterpret_cast<float*>(ws + l.sum);
+  const float* slope = reinterpret_cast<const float*>(ws + l.ds);
   WgradArgs w{};
   w.N = p.N;
   w.d = p.d;
@@ -1160,8 +1186,7 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   w.e_u = ex;
   w.e_d = ex + l.FT;
   w.s = reinterpret_cast<const float*>(ws + l.s);
-  w.ds = reinterpret_cast<const float*>(ws + l.ds);
-  w.dq = dq;
+  w.sum = sum;
   w.partial = reinterpret_cast<float*>(ws + l.part);
   {
     const size_t lds = size_t(wgrad_words(CT, BF)) * 16;
@@ -1176,7 +1201,7 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   float* part_g = reinterpret_cast<float*>(ws + l.part_g);
   if (a.grad_w_gate || a.grad_b_gate) {
     k_ffn_dwg<BF><<<dim3((l.CT * ((l.FT + 1) / 2) + 3) / 4, l.Sg), dim3(256), 0, s>>>(p.N, p.d, p.C, l.CT, l.FT, a.x,
-                                                                                     dq, part_g);
+                                                                                     sum, slope, part_g);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -1193,7 +1218,7 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
                           lds);
   if (e != hipSuccess) return e;
   k_ffn_dx0<CT, BF><<<dim3((p.N + 127) / 128, l.KS), dim3(256), lds, s>>>(
-      p.N, p.C, l.FT, dq, reinterpret_cast<const u32x4*>(ws + l.pack[4]), ex + 4 * l.FT, r0);
+      p.N, p.C, l.FT, sum, slope, reinterpret_cast<const u32x4*>(ws + l.pack[4]), ex + 4 * l.FT, r0);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   RowsArgs r{};
