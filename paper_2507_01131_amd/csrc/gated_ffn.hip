@@ -708,7 +708,7 @@ struct WgradArgs {
 
 // Waves of a workgroup: two a SIMD where a wave's packed weights and sums leave
 // room in 256 registers.  A pair of waves has one tile of 32 hidden units.
-__host__ __device__ constexpr int wgrad_waves(int CT, bool BF) { return BF || CT <= 6 ? 8 : 4; }
+__host__ __device__ constexpr int wgrad_waves(int CT, bool BF) { return BF || CT <= 4 ? 8 : 4; }
 // Operand blocks that k_ffn_wgrad writes itself: each lane half 33 words apart
 // instead of 32, so that the 4 x 4 blocks' writes spread over the LDS banks;
 // and in the transposed order channel c of a tile at place wgrad_slot(c), so
@@ -716,9 +716,13 @@ __host__ __device__ constexpr int wgrad_waves(int CT, bool BF) { return BF || CT
 // way a wave reads 32 words in some order.
 constexpr int kHalfW = 33, kBlkW = 2 * kHalfW;
 __device__ __forceinline__ int wgrad_slot(int c) { return (c & 3) * 8 + (c >> 2); }
-// LDS words: x and grad_y in both operand orders, then u and p of the pairs
-__host__ __device__ constexpr int wgrad_words(int CT, bool BF) {
-  return 4 * 2 * CT * (BF ? 1 : 2) * kBlkW + wgrad_waves(CT, BF) * 4 * kBlk;
+// nodes that a tile of 32 rows can touch
+__host__ __device__ constexpr int wgrad_nodes(int d) { return d == 1 ? 32 : 31 / d + 2; }
+// LDS words: x and grad_y in both operand orders, u and p of the pairs, and
+// (eight waves) the gate's values of two tiles' nodes
+__host__ __device__ constexpr int wgrad_words(int CT, bool BF, int d) {
+  return 4 * 2 * CT * (BF ? 1 : 2) * kBlkW + wgrad_waves(CT, BF) * 4 * kBlk +
+         (wgrad_waves(CT, BF) == 8 ? 2 * 32 * ((wgrad_nodes(d) + 1) / 2 * 2) : 0);
 }
 
 // four channels of a row as they lie in memory
@@ -745,6 +749,11 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
   __shared__ int s_eb;
   u32x4* sU = smem + 4 * kOp;                                                    // [pair][4][64]
   float* sP = reinterpret_cast<float*>(sU + wgrad_waves(CT, BF) / 2 * 4 * kBlk);  // [pair][32 rows][32]
+  // the gate's values: eight waves (256 registers) keep them in LDS, [tile
+  // parity][node][the pairs' 128 hidden units], four in registers
+  constexpr bool kGateLds = NT == 8 * kWave;
+  float* sS = sP + wgrad_waves(CT, BF) / 2 * 1024;
+  const int s_words = (wgrad_nodes(a.d) + 1) / 2 * 2 * 128;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int role = wave & 1, g = wave >> 1;  // role 0: u and grad W_down; 1: dh and grad W_up
@@ -805,10 +814,28 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     else
       return Raw4<BF>{*reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + row * C + i)};
   };
+  // the gate's values of the nodes of rows mb .. mb + 31 counted from node nb
+  auto fetch_gate = [&](int nb, int mb, int buf) {
+    const int cnt = int((uint32_t(mb + 31) * inv_d) >> 16) + 1;
+    for (int i = wave; 2 * i < cnt; i += NT / kWave) {
+      const int node = min(nb + 2 * i + h, a.N - 1);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(a.s + size_t(node) * Fp + blockIdx.x * 128 + 4 * l32),
+          (__attribute__((address_space(3))) void*)(sS + buf * s_words + 2 * i * 128), 16, 0, 0);
+    }
+  };
+  // (the places of a thread's blocks are formed anew for every tile: kept in
+  // registers over the loop they would push others out)
+  auto here = [&] {
+    int t = tid;
+    asm volatile("" : "+v"(t));
+    return t;
+  };
   auto fetch = [&](int rb) {
+    const int t0 = here();
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      const int i = tid + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
+      const int i = t0 + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const bool on = i < 64 * CT && c < C && rb + 4 * rg + r < r1;
@@ -849,9 +876,11 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     }
   };
   if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
+  int prev = 0;         // rows of the tile before, whose products wait in sP
+  int nb = n0, mb = 0;  // the tile's first row: row mb of node nb
+  int buf = 0;
+  if constexpr (kGateLds) fetch_gate(nb, mb, 0);
   fetch(r0);
-  int prev = 0;                  // rows of the tile before, whose products wait in sP
-  int nb = n0, mb = 0;           // the tile's first row: row mb of node nb
   for (int rb = r0; rb < r1; rb += 32) {
     __syncthreads();  // s_max is zero; the tile before is consumed
     if constexpr (!BF) {
@@ -889,9 +918,10 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
         if (tid == 0) s_eb = top;
       }
     }
+    const int t0 = here();
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      const int i = tid + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
+      const int i = t0 + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
       if (i < 64 * CT) {
         float sx[4], sg[4];
         if constexpr (!BF) {
@@ -905,15 +935,24 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
         put(vg[k], rg, c, smem + 2 * kOp, sg);
       }
     }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the gate's values too
     __syncthreads();
-    // the gate of this lane's hidden unit for its rows' nodes (loads
-    // end in order: before the next tile's)
+    const int nb_cur = nb, mb_cur = mb;
+    mb += 32;
+    const int step = int((uint32_t(mb) * inv_d) >> 16);
+    nb += step;
+    mb -= step * d;
+    // loads end in order: the gate's before the next tile's rows
     float s[16];
-    const float* sp = a.s + size_t(nb) * Fp + 32 * ft + l32;
+    if constexpr (kGateLds) {
+      if (rb + 32 < r1) fetch_gate(nb, mb, buf ^ 1);
+    } else {
+      const float* sp = a.s + size_t(nb_cur) * Fp + 32 * ft + l32;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int o = min(acc_row(v, h), r1 - 1 - rb);
-      s[v] = sp[int((uint32_t(mb + o) * inv_d) >> 16) * Fp];
+      for (int v = 0; v < 16; ++v) {
+        const int o = min(acc_row(v, h), r1 - 1 - rb);
+        s[v] = sp[int((uint32_t(mb_cur + o) * inv_d) >> 16) * Fp];
+      }
     }
     if (rb + 32 < r1) fetch(rb + 32);
     if constexpr (!BF)
@@ -935,10 +974,6 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
       add_rows(prev);
     }
     prev = min(32, r1 - rb);
-    mb += 32;
-    const int step = int((uint32_t(mb) * inv_d) >> 16);
-    nb += step;
-    mb -= step * d;
     __syncthreads();
     const int eb = BF ? 0 : s_eb;
 #pragma unroll
@@ -954,8 +989,15 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * k + i] *= t[4 * k + i] * rf[i];
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kGateLds) {
+          const int node = int((uint32_t(mb_cur + 8 * k + 4 * h + i) * inv_d) >> 16);
+          s[4 * k + i] = sS[buf * s_words + node * 128 + g * 32 + l32];
+        }
+        s[4 * k + i] *= t[4 * k + i] * rf[i];
+      }
     }
+    buf ^= 1;
     u32x4 o[2][P];
     to_operand<BF>(s, eb, E, o, [&](float f) {
 #pragma unroll
@@ -1189,7 +1231,7 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   w.sum = sum;
   w.partial = reinterpret_cast<float*>(ws + l.part);
   {
-    const size_t lds = size_t(wgrad_words(CT, BF)) * 16;
+    const size_t lds = size_t(wgrad_words(CT, BF, p.d)) * 16;
     auto k = k_ffn_wgrad<CT, BF>;
     e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     if (e != hipSuccess) return e;
