@@ -72,19 +72,19 @@ __device__ __forceinline__ float halves_sum(float v) {
 }
 // Steps of P operand blocks each, read from LDS kDepth - 1 steps ahead of
 // their matrix instructions: use(step, blocks).
-template <int kSteps, int P, int kDepth, typename Use>
+template <int kSteps, int P, int kDepth, int kStride = kBlk, typename Use>
 __device__ __forceinline__ void stream_blocks(const u32x4* w, Use use) {
   u32x4 ring[kDepth][P];
 #pragma unroll
   for (int i = 0; i < kDepth - 1 && i < kSteps; ++i)
 #pragma unroll
-    for (int p = 0; p < P; ++p) ring[i][p] = w[(i * P + p) * kBlk];
+    for (int p = 0; p < P; ++p) ring[i][p] = w[(i * P + p) * kStride];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     if (i + kDepth - 1 < kSteps)
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        ring[(i + kDepth - 1) % kDepth][p] = w[((i + kDepth - 1) * P + p) * kBlk];
+        ring[(i + kDepth - 1) % kDepth][p] = w[((i + kDepth - 1) * P + p) * kStride];
     __builtin_amdgcn_sched_barrier(0);
     use(i, ring[i % kDepth]);
     __builtin_amdgcn_sched_barrier(0);
@@ -721,7 +721,7 @@ __host__ __device__ constexpr int wgrad_nodes(int d) { return d == 1 ? 32 : 31 /
 // LDS words: x and grad_y in both operand orders, u and p of the pairs, and
 // (eight waves) the gate's values of two tiles' nodes
 __host__ __device__ constexpr int wgrad_words(int CT, bool BF, int d) {
-  return 4 * 2 * CT * (BF ? 1 : 2) * kBlkW + wgrad_waves(CT, BF) * 4 * kBlk +
+  return 4 * 2 * CT * (BF ? 1 : 2) * kBlkW + wgrad_waves(CT, BF) * (2 * kBlk + 256) +
          (wgrad_waves(CT, BF) == 8 ? 2 * 32 * ((wgrad_nodes(d) + 1) / 2 * 2) : 0);
 }
 
@@ -735,7 +735,7 @@ struct Raw4<true> {
   uint2 v;
 };
 
-template <int CT, bool BF>
+template <int CT, bool BF, bool AL>
 __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     __attribute__((amdgpu_waves_per_eu(wgrad_waves(CT, BF) / 4, wgrad_waves(CT, BF) / 4))) void k_ffn_wgrad(
         WgradArgs a) {
@@ -747,12 +747,13 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
   __shared__ uint32_t s_max[2][32];
   __shared__ float s_rowf[32];
   __shared__ int s_eb;
-  u32x4* sU = smem + 4 * kOp;                                                    // [pair][4][64]
-  float* sP = reinterpret_cast<float*>(sU + wgrad_waves(CT, BF) / 2 * 4 * kBlk);  // [pair][32 rows][32]
+  u32x4* sU = smem + 4 * kOp;  // [pair][4][64]
+  // [tile parity][pair][8 groups of four rows][32]
+  f32x4* sP = reinterpret_cast<f32x4*>(sU + wgrad_waves(CT, BF) / 2 * 4 * kBlk);
   // the gate's values: eight waves (256 registers) keep them in LDS, [tile
   // parity][node][the pairs' 128 hidden units], four in registers
-  constexpr bool kGateLds = NT == 8 * kWave;
-  float* sS = sP + wgrad_waves(CT, BF) / 2 * 1024;
+  constexpr bool kGateLds = !AL && NT == 8 * kWave;
+  float* sS = reinterpret_cast<float*>(sP + wgrad_waves(CT, BF) * 256);
   const int s_words = (wgrad_nodes(a.d) + 1) / 2 * 2 * 128;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -788,22 +789,26 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
   float run = 0.f;
   int in_node = 0, node = n0;
   const bool sums = own && h == 0;
-  auto add_rows = [&](int n) {  // the first n rows of sP
-    const float* p = sP + g * 1024 + l32;
-    for (int q = 0; q < n; q += 8) {
-      float v[8];
+  auto node_done = [&] {
+    if (sums) a.sum[size_t(node) * Fp + 32 * ft + l32] = run;
+    run = 0.f;
+    in_node = 0;
+    ++node;
+  };
+  auto add_rows = [&](const f32x4* p, int n) {  // the first n rows of p
+    for (int q = 0; 4 * q < n; ++q) {
+      const f32x4 v = p[q * 32];
+      if (4 * q + 4 <= n && in_node + 4 <= d) {  // (rows added in order on either way)
+        run = (((run + v[0]) + v[1]) + v[2]) + v[3];
+        in_node += 4;
+        if (in_node == d) node_done();
+      } else {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] = p[(q + r) * 32];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        if (q + r >= n) break;
-        run += v[r];
-        if (++in_node == d) {
-          if (sums) a.sum[size_t(node) * Fp + 32 * ft + l32] = run;
-          run = 0.f;
-          in_node = 0;
-          ++node;
-        }
+        for (int r = 0; r < 4; ++r)
+          if (4 * q + r < n) {
+            run += v[r];
+            if (++in_node == d) node_done();
+          }
       }
     }
   };
@@ -831,14 +836,14 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     asm volatile("" : "+v"(t));
     return t;
   };
-  auto fetch = [&](int rb) {
+  auto fetch = [&](int rb, int n) {  // rows rb .. rb + n - 1 of a tile
     const int t0 = here();
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
       const int i = t0 + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const bool on = i < 64 * CT && c < C && rb + 4 * rg + r < r1;
+        const bool on = i < 64 * CT && c < C && 4 * rg + r < n;
         const uint32_t at = 4 * rg * C + c;
         vx[k][r] = on ? raw(a.x, size_t(rb + r), at) : Raw4<BF>{};
         vg[k][r] = on ? raw(a.gy, size_t(rb + r), at) : Raw4<BF>{};
@@ -879,9 +884,24 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
   int prev = 0;         // rows of the tile before, whose products wait in sP
   int nb = n0, mb = 0;  // the tile's first row: row mb of node nb
   int buf = 0;
+  // Aligned tiles: one node's rows (d = 25), half of them (36, 49) or two
+  // nodes' (16); the other rows of a tile are zero.
+  const int part_rows = d > 32 ? (d + 1) / 2 : (d == 16 ? 32 : d);
+  auto tile_rows = [&](int rb, int mb) {
+    return AL ? min(part_rows, d == 16 ? r1 - rb : d - mb) : min(32, r1 - rb);
+  };
+  // the gate of this lane's hidden unit for rows 0 .. 15 and 16 .. 31 of a tile
+  auto gate_of = [&](int node, int second) {
+    return a.s[size_t(min(node + (d == 16 ? second : 0), n1 - 1)) * Fp + 32 * ft + l32];
+  };
+  float s_cur[2] = {0.f, 0.f}, s_nxt[2] = {0.f, 0.f}, node_sum = 0.f;
+  if constexpr (AL)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) s_nxt[i] = gate_of(n0, i);
   if constexpr (kGateLds) fetch_gate(nb, mb, 0);
-  fetch(r0);
-  for (int rb = r0; rb < r1; rb += 32) {
+  int rows = tile_rows(r0, 0);
+  fetch(r0, rows);
+  for (int rb = r0; rb < r1;) {
     __syncthreads();  // s_max is zero; the tile before is consumed
     if constexpr (!BF) {
 #pragma unroll
@@ -937,44 +957,51 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the gate's values too
     __syncthreads();
-    const int nb_cur = nb, mb_cur = mb;
-    mb += 32;
-    const int step = int((uint32_t(mb) * inv_d) >> 16);
+    const int nb_cur = nb, mb_cur = mb, rb_cur = rb, rows_cur = rows;
+    mb += rows;
+    const int step = AL ? (d == 16 ? 2 : mb / d) : int((uint32_t(mb) * inv_d) >> 16);
     nb += step;
-    mb -= step * d;
+    mb = AL && d == 16 ? 0 : mb - step * d;
+    rb += rows;
+    const bool more = rb < r1;
+    if (more) rows = tile_rows(rb, mb);
     // loads end in order: the gate's before the next tile's rows
     float s[16];
-    if constexpr (kGateLds) {
-      if (rb + 32 < r1) fetch_gate(nb, mb, buf ^ 1);
+    if constexpr (AL) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s_cur[i] = s_nxt[i];
+        if (more) s_nxt[i] = gate_of(nb, i);
+      }
+    } else if constexpr (kGateLds) {
+      if (more) fetch_gate(nb, mb, buf ^ 1);
     } else {
       const float* sp = a.s + size_t(nb_cur) * Fp + 32 * ft + l32;
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const int o = min(acc_row(v, h), r1 - 1 - rb);
+        const int o = min(acc_row(v, h), r1 - 1 - rb_cur);
         s[v] = sp[int((uint32_t(mb_cur + o) * inv_d) >> 16) * Fp];
       }
     }
-    if (rb + 32 < r1) fetch(rb + 32);
+    if (more) fetch(rb, rows);
     if constexpr (!BF)
       if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
     // u or dh of the tile: rows in registers, hidden units in lanes
     f32x16 t = f32x16{};
-#pragma unroll
-    for (int st = 0; st < 2 * CT; ++st) {
-      u32x4 op[P];
-#pragma unroll
-      for (int p = 0; p < P; ++p) op[p] = rows_op[(st * P + p) * kBlkW];
-      t = mm_parts<BF>(op, w[st], t);
-    }
+    stream_blocks<2 * CT, P, 3, kBlkW>(rows_op, [&](int st, const u32x4* op) { t = mm_parts<BF>(op, w[st], t); });
     if (role == 0) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         sU[(g * 4 + k) * kBlk + lane] =
             __builtin_bit_cast(u32x4, f32x4{t[4 * k], t[4 * k + 1], t[4 * k + 2], t[4 * k + 3]});
-      add_rows(prev);
     }
-    prev = min(32, r1 - rb);
     __syncthreads();
+    // products of the two tiles' parities apart: role 0 sums the tile before
+    // while role 1 writes this one's
+    f32x4* p_own = sP + ((buf * (wgrad_waves(CT, BF) / 2) + g) * 8) * 32 + l32;
+    if (!AL && role == 0) add_rows(sP + (((buf ^ 1) * (wgrad_waves(CT, BF) / 2) + g) * 8) * 32 + l32, prev);
+    prev = rows_cur;
+    float psum[2] = {0.f, 0.f};
     const int eb = BF ? 0 : s_eb;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -982,11 +1009,14 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
       const f32x4 rf = BF ? f32x4{1.f, 1.f, 1.f, 1.f} : *reinterpret_cast<const f32x4*>(s_rowf + 8 * k + 4 * h);
       if (role == 1) {
         const f32x4 u = __builtin_bit_cast(f32x4, sU[(g * 4 + k) * kBlk + lane]);
+        f32x4 p;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p = u[i] * rf[i] * t[4 * k + i];
-          sP[(g * 32 + 8 * k + 4 * h + i) * 32 + l32] = BF ? p : ldexpf(p, eb + e_both);
+          p[i] = u[i] * rf[i] * t[4 * k + i];
+          if constexpr (!BF && !AL) p[i] = ldexpf(p[i], eb + e_both);
+          if constexpr (AL) psum[k >> 1] += p[i];
         }
+        if constexpr (!AL) p_own[(2 * k + h) * 32] = p;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -994,27 +1024,39 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
           const int node = int((uint32_t(mb_cur + 8 * k + 4 * h + i) * inv_d) >> 16);
           s[4 * k + i] = sS[buf * s_words + node * 128 + g * 32 + l32];
         }
+        if constexpr (AL) s[4 * k + i] = s_cur[k >> 1];
         s[4 * k + i] *= t[4 * k + i] * rf[i];
       }
     }
     buf ^= 1;
+    if (AL && role == 1) {
+      // the node's sum: both halves' rows; two nodes at d = 16, two tiles' parts above 32
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        psum[i] = halves_sum(psum[i]);
+        if constexpr (!BF) psum[i] = ldexpf(psum[i], eb + e_both);
+      }
+      float* out = a.sum + size_t(nb_cur) * Fp + 32 * ft + l32;
+      if (d == 16) {
+        if (own && nb_cur + h < n1) out[h * Fp] = h ? psum[1] : psum[0];
+      } else {
+        node_sum += psum[0] + psum[1];
+        if (mb == 0) {
+          if (own && h == 0) *out = node_sum;
+          node_sum = 0.f;
+        }
+      }
+    }
     u32x4 o[2][P];
     to_operand<BF>(s, eb, E, o, [&](float f) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) acc[ct] *= f;
     });
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32x4 op[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) op[p] = cols_op[((2 * ct + q) * P + p) * kBlkW];
-        acc[ct] = mm_parts<BF>(op, o[q], acc[ct]);
-      }
+    stream_blocks<2 * CT, P, 3, kBlkW>(
+        cols_op, [&](int i, const u32x4* op) { acc[i >> 1] = mm_parts<BF>(op, o[i & 1], acc[i >> 1]); });
   }
   __syncthreads();
-  if (role == 0) add_rows(prev);
+  if (!AL && role == 0) add_rows(sP + (((buf ^ 1) * (wgrad_waves(CT, BF) / 2) + g) * 8) * 32 + l32, prev);
   if (!own) return;
   float* out = a.partial + (size_t(blockIdx.y) * 2 + role) * C * Fp + 32 * ft + l32;
 #pragma unroll
@@ -1232,7 +1274,9 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   w.partial = reinterpret_cast<float*>(ws + l.part);
   {
     const size_t lds = size_t(wgrad_words(CT, BF, p.d)) * 16;
-    auto k = k_ffn_wgrad<CT, BF>;
+    // tiles of whole nodes where a node's rows fill most of one: no sums of
+    // rows through LDS and one value of the gate a lane
+    auto k = p.d >= 16 ? k_ffn_wgrad<CT, BF, true> : k_ffn_wgrad<CT, BF, false>;
     e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     if (e != hipSuccess) return e;
     const int per = wgrad_waves(CT, BF) / 2;
