@@ -706,9 +706,14 @@ struct WgradArgs {
   float* partial;                 // [gridDim.y][2][C][32 FT]: W_down's (as [c][f]), then W_up's
 };
 
-// Waves of a workgroup: two a SIMD where a wave's packed weights and sums leave
-// room in 256 registers.  A pair of waves has one tile of 32 hidden units.
-__host__ __device__ constexpr int wgrad_waves(int CT, bool BF) { return BF || CT <= 4 ? 8 : 4; }
+// Eight waves, two a SIMD: a wave's packed weights and sums fit 256 registers
+// with a pair of waves to a tile of 32 hidden units up to 128 fp32 channels
+// (256 bf16 ones).  Above, four waves share a tile: each role's two take half
+// of the contraction over channels, exchange the halves of u and dh through
+// LDS, and take half of the channels of the sums.
+constexpr int kWgradWaves = 8;
+__host__ __device__ constexpr bool wgrad_halves(int CT, bool BF) { return !BF && CT > 4; }
+__host__ __device__ constexpr int wgrad_tiles(int CT, bool BF) { return wgrad_halves(CT, BF) ? 2 : 4; }
 // Operand blocks that k_ffn_wgrad writes itself: each lane half 33 words apart
 // instead of 32, so that the 4 x 4 blocks' writes spread over the LDS banks;
 // and in the transposed order channel c of a tile at place wgrad_slot(c), so
@@ -718,11 +723,12 @@ constexpr int kHalfW = 33, kBlkW = 2 * kHalfW;
 __device__ __forceinline__ int wgrad_slot(int c) { return (c & 3) * 8 + (c >> 2); }
 // nodes that a tile of 32 rows can touch
 __host__ __device__ constexpr int wgrad_nodes(int d) { return d == 1 ? 32 : 31 / d + 2; }
-// LDS words: x and grad_y in both operand orders, u and p of the pairs, and
-// (eight waves) the gate's values of two tiles' nodes
+// LDS words: x and grad_y in both operand orders, then u (with halves, in the
+// place of the operands in row order) and p of the tiles, and (without halves)
+// the gate's values of two tiles' nodes
 __host__ __device__ constexpr int wgrad_words(int CT, bool BF, int d) {
-  return 4 * 2 * CT * (BF ? 1 : 2) * kBlkW + wgrad_waves(CT, BF) * (2 * kBlk + 256) +
-         (wgrad_waves(CT, BF) == 8 ? 2 * 32 * ((wgrad_nodes(d) + 1) / 2 * 2) : 0);
+  return 4 * 2 * CT * (BF ? 1 : 2) * kBlkW + wgrad_tiles(CT, BF) * 512 +
+         (wgrad_halves(CT, BF) ? 0 : wgrad_tiles(CT, BF) * 4 * kBlk + 2 * 32 * ((wgrad_nodes(d) + 1) / 2 * 2));
 }
 
 // four channels of a row as they lie in memory
@@ -736,10 +742,12 @@ struct Raw4<true> {
 };
 
 template <int CT, bool BF, bool AL>
-__global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
-    __attribute__((amdgpu_waves_per_eu(wgrad_waves(CT, BF) / 4, wgrad_waves(CT, BF) / 4))) void k_ffn_wgrad(
-        WgradArgs a) {
-  constexpr int P = BF ? 1 : 2, NT = wgrad_waves(CT, BF) * kWave;
+__global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_ffn_wgrad(
+    WgradArgs a) {
+  constexpr int P = BF ? 1 : 2, NT = kWgradWaves * kWave, kTiles = wgrad_tiles(CT, BF);
+  constexpr bool kHalves = wgrad_halves(CT, BF);
+  constexpr int kSteps = kHalves ? CT : 2 * CT;        // of a wave's contraction over channels
+  constexpr int kCt = kHalves ? (CT + 1) / 2 : CT;     // channel tiles of a wave's sums
   constexpr int kOp = 2 * CT * P * kBlkW;  // words of a tensor in one operand order
   constexpr int kPack = 2 * CT * P * kBlk;  // of a packed tile
   constexpr int kItems = (64 * CT + NT - 1) / NT;  // 4 x 4 blocks of a 32-row tile per thread and tensor
@@ -747,40 +755,44 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
   __shared__ uint32_t s_max[2][32];
   __shared__ float s_rowf[32];
   __shared__ int s_eb;
-  u32x4* sU = smem + 4 * kOp;  // [pair][4][64]
-  // [tile parity][pair][8 groups of four rows][32]
-  f32x4* sP = reinterpret_cast<f32x4*>(sU + wgrad_waves(CT, BF) / 2 * 4 * kBlk);
-  // the gate's values: eight waves (256 registers) keep them in LDS, [tile
-  // parity][node][the pairs' 128 hidden units], four in registers
-  constexpr bool kGateLds = !AL && NT == 8 * kWave;
-  float* sS = reinterpret_cast<float*>(sP + wgrad_waves(CT, BF) * 256);
+  u32x4* sU = kHalves ? smem : smem + 4 * kOp;  // [wave of role 0, or every wave][4][64]
+  static_assert(!kHalves || 2 * kOp >= kWgradWaves * 4 * kBlk, "the halves fit the operands in row order");
+  // [tile parity][tile of hidden units][8 groups of four rows][32]
+  f32x4* sP = reinterpret_cast<f32x4*>(smem + 4 * kOp + (kHalves ? 0 : kTiles * 4 * kBlk));
+  // the gate's values: without halves in LDS, [tile parity][node][the tiles'
+  // 128 hidden units], else in registers
+  constexpr bool kGateLds = !AL && !kHalves;
+  float* sS = reinterpret_cast<float*>(sP + kTiles * 512);
   const int s_words = (wgrad_nodes(a.d) + 1) / 2 * 2 * 128;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int role = wave & 1, g = wave >> 1;  // role 0: u and grad W_down; 1: dh and grad W_up
+  // role 0: u and grad W_down; 1: dh and grad W_up
+  const int hf = kHalves ? wave & 1 : 0, role = (kHalves ? wave >> 1 : wave) & 1, g = wave / (kHalves ? 4 : 2);
   const int C = a.C, d = a.d, FT = a.FT, Fp = 32 * FT;
   const int n0 = int(int64_t(blockIdx.y) * a.N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * a.N / gridDim.y);
   const int r0 = n0 * d, r1 = n1 * d;
-  // a pair without a tile of its own repeats the last one and stores nothing
-  const int tile = blockIdx.x * (wgrad_waves(CT, BF) / 2) + g, ft = min(tile, FT - 1);
+  // waves without a tile of their own repeat the last one and store nothing
+  const int tile = blockIdx.x * kTiles + g, ft = min(tile, FT - 1);
   const bool own = tile < FT;
-  u32x4 w[2 * CT][P];
+  u32x4 w[kSteps][P];
   {
-    const u32x4* src = (role == 0 ? a.up_u : a.up_d) + size_t(ft) * kPack + lane;
+    const u32x4* src = (role == 0 ? a.up_u : a.up_d) + size_t(ft) * kPack + hf * kSteps * P * kBlk + lane;
 #pragma unroll
-    for (int st = 0; st < 2 * CT; ++st)
+    for (int st = 0; st < kSteps; ++st)
 #pragma unroll
       for (int p = 0; p < P; ++p) w[st][p] = src[(st * P + p) * kBlk];
   }
   const int e_own = BF ? 0 : (role == 0 ? a.e_u : a.e_d)[ft], e_both = BF ? 0 : a.e_u[ft] + a.e_d[ft];
-  // LDS: x in row order, x in transposed order, then grad_y in both
-  const u32x4* rows_op = smem + (role == 0 ? 0 : 2) * kOp + h * kHalfW + l32;  // x for u, grad_y for dh
+  // LDS: x and grad_y in row order, then both in transposed order
+  // x for u, grad_y for dh
+  const u32x4* rows_op = smem + (role == 0 ? 0 : 1) * kOp + hf * kSteps * P * kBlkW + h * kHalfW + l32;
   // grad_y for W_down, x for W_up
-  const u32x4* cols_op = smem + (role == 0 ? 3 : 1) * kOp + h * kHalfW + wgrad_slot(l32);
-  f32x16 acc[CT];
+  const u32x4* cols_op =
+      smem + (role == 0 ? 3 : 2) * kOp + hf * kCt * 2 * P * kBlkW + h * kHalfW + wgrad_slot(l32);
+  f32x16 acc[kCt];
   int E = kUnset;
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x16{};
+  for (int ct = 0; ct < kCt; ++ct) acc[ct] = f32x16{};
   // rows to nodes without a division: (row - first row of node nb) / d for
   // values up to d + 31 <= 80, as a product with ceil(2^16 / d) (exact there)
   const uint32_t inv_d = (65536u + d - 1) / d;
@@ -875,7 +887,7 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
         const int k = cc >> 1, sh = 16 * (cc & 1);
         const uint32_t lo = ((hl[p][0][k] >> sh) & 0xffffu) | ((hl[p][1][k] >> sh) << 16);
         const uint32_t hi = ((hl[p][2][k] >> sh) & 0xffffu) | ((hl[p][3][k] >> sh) << 16);
-        reinterpret_cast<uint2*>(op + kOp + ((2 * ct + q) * P + p) * kBlkW + ht * kHalfW +
+        reinterpret_cast<uint2*>(op + 2 * kOp + ((2 * ct + q) * P + p) * kBlkW + ht * kHalfW +
                                  wgrad_slot((c + cc) & 31))[it] = uint2{lo, hi};
       }
     }
@@ -952,7 +964,7 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
           }
         }
         put(vx[k], rg, c, smem, sx);
-        put(vg[k], rg, c, smem + 2 * kOp, sg);
+        put(vg[k], rg, c, smem + kOp, sg);
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the gate's values too
@@ -988,18 +1000,28 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
       if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
     // u or dh of the tile: rows in registers, hidden units in lanes
     f32x16 t = f32x16{};
-    stream_blocks<2 * CT, P, 3, kBlkW>(rows_op, [&](int st, const u32x4* op) { t = mm_parts<BF>(op, w[st], t); });
-    if (role == 0) {
+    stream_blocks<kSteps, P, 3, kBlkW>(rows_op, [&](int st, const u32x4* op) { t = mm_parts<BF>(op, w[st], t); });
+    if constexpr (kHalves) __syncthreads();  // the operands in row order are consumed: the halves take their place
+    u32x4* u_own = sU + (kHalves ? wave : g) * 4 * kBlk + lane;
+    if (kHalves || role == 0) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        sU[(g * 4 + k) * kBlk + lane] =
-            __builtin_bit_cast(u32x4, f32x4{t[4 * k], t[4 * k + 1], t[4 * k + 2], t[4 * k + 3]});
+        u_own[k * kBlk] = __builtin_bit_cast(u32x4, f32x4{t[4 * k], t[4 * k + 1], t[4 * k + 2], t[4 * k + 3]});
     }
     __syncthreads();
+    if constexpr (kHalves) {
+      const u32x4* other = sU + (wave ^ 1) * 4 * kBlk + lane;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const f32x4 v = __builtin_bit_cast(f32x4, other[k * kBlk]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[4 * k + i] += v[i];
+      }
+    }
     // products of the two tiles' parities apart: role 0 sums the tile before
     // while role 1 writes this one's
-    f32x4* p_own = sP + ((buf * (wgrad_waves(CT, BF) / 2) + g) * 8) * 32 + l32;
-    if (!AL && role == 0) add_rows(sP + (((buf ^ 1) * (wgrad_waves(CT, BF) / 2) + g) * 8) * 32 + l32, prev);
+    f32x4* p_own = sP + (buf * kTiles + g) * 256 + l32;
+    if (!AL && role == 0 && hf == 0) add_rows(sP + ((buf ^ 1) * kTiles + g) * 256 + l32, prev);
     prev = rows_cur;
     float psum[2] = {0.f, 0.f};
     const int eb = BF ? 0 : s_eb;
@@ -1007,8 +1029,9 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     for (int k = 0; k < 4; ++k) {
       // rows 8 k + 4 h .. + 3
       const f32x4 rf = BF ? f32x4{1.f, 1.f, 1.f, 1.f} : *reinterpret_cast<const f32x4*>(s_rowf + 8 * k + 4 * h);
-      if (role == 1) {
-        const f32x4 u = __builtin_bit_cast(f32x4, sU[(g * 4 + k) * kBlk + lane]);
+      if (role == 1 && hf == 0) {
+        f32x4 u = __builtin_bit_cast(f32x4, sU[(kHalves ? 4 * g : g) * 4 * kBlk + k * kBlk + lane]);
+        if constexpr (kHalves) u += __builtin_bit_cast(f32x4, sU[(4 * g + 1) * 4 * kBlk + k * kBlk + lane]);
         f32x4 p;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -1029,7 +1052,7 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
       }
     }
     buf ^= 1;
-    if (AL && role == 1) {
+    if (AL && role == 1 && hf == 0) {
       // the node's sum: both halves' rows; two nodes at d = 16, two tiles' parts above 32
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -1050,20 +1073,22 @@ __global__ __launch_bounds__(wgrad_waves(CT, BF)* kWave)
     u32x4 o[2][P];
     to_operand<BF>(s, eb, E, o, [&](float f) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) acc[ct] *= f;
+      for (int ct = 0; ct < kCt; ++ct) acc[ct] *= f;
     });
-    stream_blocks<2 * CT, P, 3, kBlkW>(
+    // (the last channel tile of the second half repeats one where their number
+    // is odd: it stays in LDS and is not stored)
+    stream_blocks<2 * kCt, P, 3, kBlkW>(
         cols_op, [&](int i, const u32x4* op) { acc[i >> 1] = mm_parts<BF>(op, o[i & 1], acc[i >> 1]); });
   }
   __syncthreads();
-  if (!AL && role == 0) add_rows(sP + (((buf ^ 1) * (wgrad_waves(CT, BF) / 2) + g) * 8) * 32 + l32, prev);
+  if (!AL && role == 0 && hf == 0) add_rows(sP + ((buf ^ 1) * kTiles + g) * 256 + l32, prev);
   if (!own) return;
   float* out = a.partial + (size_t(blockIdx.y) * 2 + role) * C * Fp + 32 * ft + l32;
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
+  for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      const int c = 32 * ct + acc_row(v, h);
+      const int c = 32 * (hf * kCt + ct) + acc_row(v, h);
       if (c < C) out[size_t(c) * Fp] = BF ? acc[ct][v] : ldexpf(acc[ct][v], E + e_own);
     }
 }
@@ -1147,7 +1172,7 @@ Layout layout(const FfnShape& p, bool backward) {
     l.KS = std::min({4, l.FT, std::max(1, device_cus() / ((p.N + 127) / 128 + 1))});
     o += al256(size_t(l.KS) * p.N * p.C * 4);
     // one workgroup a CU over the ranges of rows; a range has a node at least
-    const int per = wgrad_waves(l.CT, p.bf16) / 2, fb = (l.FT + per - 1) / per;
+    const int per = wgrad_tiles(l.CT, p.bf16), fb = (l.FT + per - 1) / per;
     const int most = device_cus() / fb;
     l.S = p.N < most ? p.N : (most > 1 ? most : 1);
     if (l.S < 1) l.S = 1;
@@ -1279,8 +1304,8 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
     auto k = p.d >= 16 ? k_ffn_wgrad<CT, BF, true> : k_ffn_wgrad<CT, BF, false>;
     e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     if (e != hipSuccess) return e;
-    const int per = wgrad_waves(CT, BF) / 2;
-    k<<<dim3((l.FT + per - 1) / per, l.S), dim3(wgrad_waves(CT, BF) * kWave), lds, s>>>(w);
+    const int per = wgrad_tiles(CT, BF);
+    k<<<dim3((l.FT + per - 1) / per, l.S), dim3(kWgradWaves * kWave), lds, s>>>(w);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
