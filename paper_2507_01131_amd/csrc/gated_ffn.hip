@@ -381,6 +381,7 @@ struct RowsArgs {
   const float* residual0;    // [n_res0, M / d, C], added to the degree-0 rows, or nullptr
   int n_res0;
   void* out;                 // [M, C]
+  float* partial;            // [gridDim.y, M, C] where the tiles of F are shared out (gridDim.y > 1)
 };
 
 // Waves a SIMD: two where a wave's rows and sums leave room in 256 registers.
@@ -391,7 +392,9 @@ __host__ __device__ constexpr int rows_waves(int CT, bool BF, int NB) {
 // A workgroup takes 4 x 32 NB rows.  The packed weights come into LDS by
 // direct loads one tile of F ahead of their use, and u of the next tile is
 // formed beside the conversion of this tile's h, so that neither the loads
-// nor the vector work stand between the matrix instructions.
+// nor the vector work stand between the matrix instructions.  With gridDim.y
+// > 1 the workgroups of one y take a share of the tiles, and k_ffn_join adds
+// their sums.
 template <int CT, bool BF, int NB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(CT, BF, NB)))) void k_ffn_rows(
     RowsArgs a) {
@@ -403,7 +406,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
   __shared__ int s_bias[kMaxFfnTiles];                    // the tiles' exponents, of both weights
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int C = a.C, FT = a.FT;
+  const int C = a.C, Fp = 32 * a.FT;
+  const int f0 = blockIdx.y * a.FT / gridDim.y, f1 = (blockIdx.y + 1) * a.FT / gridDim.y;
   auto fetch = [&](const u32x4* packed, int ft, int buf) {
     const u32x4* src = packed + size_t(ft) * kHalf;
     u32x4* dst = sw + buf * kHalf;
@@ -411,11 +415,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
     if constexpr (CT * P % 2 == 1)  // an odd pair of blocks is left
       if (wave < 2) blocks_to_lds<1>(src + 4 * (CT * P / 2) * kBlk, dst + 4 * (CT * P / 2) * kBlk, wave, lane);
   };
-  fetch(a.up, 0, 0);
-  if (FT > 1) fetch(a.up, 1, 1);
-  fetch(a.down, 0, 2);
+  // (buffers go by the parity of the tile's place in the share)
+  fetch(a.up, f0, 0);
+  if (f0 + 1 < f1) fetch(a.up, f0 + 1, 1);
+  fetch(a.down, f0, 2);
   if constexpr (!BF)
-    for (int i = threadIdx.x; i < FT; i += 256) s_bias[i] = a.e_up[i] + a.e_down[i];
+    for (int i = f0 + threadIdx.x; i < f1; i += 256) s_bias[i] = a.e_up[i] + a.e_down[i];
   int row[NB], ex[NB], E[NB];
   const float* s[NB];
   u32x4 xo[NB][2 * CT][P];
@@ -427,9 +432,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
     const bool on = row[b] < a.M;
     const int r = on ? row[b] : a.M - 1;
     ex[b] = load_row<CT, BF>(a.in, on, size_t(r) * C, C, h, xo[b]);
-    s[b] = a.s + size_t(r / a.d) * 32 * FT + 4 * h;
+    s[b] = a.s + size_t(r / a.d) * Fp + 4 * h;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 8 * k);
+    for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 32 * f0 + 8 * k);
     E[b] = kUnset;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) y[b][ct] = f32x16{};
@@ -451,10 +456,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
   };
   lds_loads_done();
   up_product(0, [](int) {});
-  for (int ft = 0; ft < FT; ++ft) {
+  for (int ft = f0; ft < f1; ++ft) {
+    const int odd = (ft - f0) & 1;
     lds_loads_done();  // W_up of tile ft + 1 and W_down of tile ft; the buffers used before are free
-    if (ft + 2 < FT) fetch(a.up, ft + 2, ft & 1);
-    if (ft + 1 < FT) fetch(a.down, ft + 1, 2 + ((ft + 1) & 1));
+    if (ft + 2 < f1) fetch(a.up, ft + 2, odd);
+    if (ft + 1 < f1) fetch(a.down, ft + 1, 2 + (odd ^ 1));
     const int bias = BF ? 0 : s_bias[ft];
     u32x4 ho[NB][2][P];
     float t[NB][16], sc[NB];
@@ -475,8 +481,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
         for (int i = 0; i < 8; ++i)
           if (i * 2 * CT / 8 == st) operand_pair<BF>(t[b], sc[b], i, ho[b]);
     };
-    if (ft + 1 < FT) {
-      up_product((ft + 1) & 1, convert);
+    if (ft + 1 < f1) {
+      up_product(odd ^ 1, convert);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -485,7 +491,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
 #pragma unroll
       for (int st = 0; st < 2 * CT; ++st) convert(st);
     }
-    stream_blocks<2 * CT, P, kDepth>(sw + (2 + (ft & 1)) * kHalf + lane, [&](int i, const u32x4* wa) {
+    stream_blocks<2 * CT, P, kDepth>(sw + (2 + odd) * kHalf + lane, [&](int i, const u32x4* wa) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) y[b][i >> 1] = mm_parts<BF>(wa, ho[b][i & 1], y[b][i >> 1]);
     });
@@ -500,6 +506,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int v = 0; v < 16; ++v) y[b][ct][v] = ldexpf(y[b][ct][v], e);
+    if (gridDim.y > 1) {
+      float* out = a.partial + (size_t(blockIdx.y) * a.M + row[b]) * C + 4 * h;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (32 * ct + 8 * k + 4 * h < C)
+            *reinterpret_cast<f32x4*>(out + 32 * ct + 8 * k) =
+                f32x4{y[b][ct][4 * k], y[b][ct][4 * k + 1], y[b][ct][4 * k + 2], y[b][ct][4 * k + 3]};
+      continue;
+    }
     if (a.residual0 && n * a.d == row[b])
       for (int p = 0; p < a.n_res0; ++p) {
         const float* r0 = a.residual0 + (size_t(p) * (a.M / a.d) + n) * C + 4 * h;
@@ -525,14 +542,33 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
   }
 }
 
+// The shares' sums in order, with the residuals, four channels a thread.
+template <bool BF>
+__global__ __launch_bounds__(256) void k_ffn_join(RowsArgs a, int n_part) {
+  const size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * 4, total = size_t(a.M) * a.C;
+  if (i >= total) return;
+  f32x4 v = f32x4{};
+#pragma unroll 4
+  for (int p = 0; p < n_part; ++p) v += *reinterpret_cast<const f32x4*>(a.partial + p * total + i);
+  if (a.residual) v += load4<BF>(a.residual, i);
+  if (a.residual0) {
+    const int row = int(i / a.C), n = row / a.d;
+    const size_t c = i - size_t(row) * a.C;
+    if (n * a.d == row)
+      for (int p = 0; p < a.n_res0; ++p)
+        v += *reinterpret_cast<const f32x4*>(a.residual0 + (size_t(p) * (a.M / a.d) + n) * a.C + c);
+  }
+  store4<BF>(a.out, i, v);
+}
+
 // ------------------------------------------------------ the gate's gradients
 // r0 = dq W_gate^T, the sums over gridDim.y shares of F apart: [gridDim.y, N, C].
 // A workgroup takes 128 nodes; the packed weights go through LDS as in
 // k_ffn_rows.
 template <int CT, bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const float* __restrict__ sum,
-                                                 const float* __restrict__ slope, const u32x4* __restrict__ wg, const int* __restrict__ eg,
-                                                 float* __restrict__ r0) {
+                                                 const float* __restrict__ slope, const u32x4* __restrict__ wg,
+                                                 const int* __restrict__ eg, float* __restrict__ r0) {
   constexpr int P = BF ? 1 : 2, kHalf = 2 * CT * P * kBlk;
   extern __shared__ u32x4 sw[];  // [2][kHalf]
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
@@ -599,21 +635,36 @@ __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const flo
     }
 }
 
+// Eight floats in three bf16 parts (to 2^-24 of each: bf16 keeps float's range,
+// so nothing has to be scaled), as one K-step's operand each.
+__device__ __forceinline__ void bf16_parts(float (&v)[8], u32x4 (&op)[3]) {
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      op[p][k] = pack_bf16x2_rne(v[2 * k], v[2 * k + 1]);
+      v[2 * k] -= __uint_as_float(op[p][k] << 16);
+      v[2 * k + 1] -= __uint_as_float(op[p][k] & 0xffff0000u);
+    }
+}
+
 // grad W_gate = x[:, 0]^T dq: a wave takes 32 channels and two tiles of hidden
-// units over a range of nodes, sixteen nodes a step with the next step's loads
-// in flight; 32x32x2 fp32 MFMA, or 32x32x16 bf16 MFMA over three bf16 parts of
-// dq (to 2^-24: nothing of it is rounded away).  The waves of the first channel
-// tile also sum dq (grad b).  partial [S][C + 1][32 FT]: the last row is grad b.
+// units over a range of nodes, sixteen nodes a step (lane half h the nodes 8 h
+// .. 8 h + 7) with the next step's loads in flight; 32x32x16 bf16 MFMA over
+// the bf16 parts of dq and of fp32 features, the products down to 2^-16 of the
+// first (six for fp32, three for bf16).  The waves of the first channel tile
+// also sum dq (grad b).  partial [S][C + 1][32 FT]: the last row is grad b.
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, int FT, const void* __restrict__ x,
                                                  const float* __restrict__ row_sum, const float* __restrict__ slope,
                                                  float* __restrict__ partial) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, l32 = lane & 31;
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int FP = (FT + 1) / 2, t = blockIdx.x * 4 + wave;
   if (t >= CT * FP) return;
   const int ct = t / FP, ft = 2 * (t - ct * FP), c = 32 * ct + l32, Fp = 32 * FT;
   const int n0 = int(int64_t(blockIdx.y) * N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * N / gridDim.y);
-  const bool two = ft + 1 < FT;
+  const bool two = ft + 1 < FT, in_c = c < C;
   f32x16 acc[2] = {f32x16{}, f32x16{}};
   float sum[2] = {0.f, 0.f};
   struct Step {
@@ -621,64 +672,60 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
     float a[8];
     uint16_t ab[8];
   };
-  // value k of a lane: node 8 h + k (bf16: the K order of the step) or 2 k + h
+  // nodes n .. n + 15; behind the range's end zeros (of the last node's address)
   auto load = [&](int n, Step& s) {
+    const float* rs = row_sum + size_t(n) * Fp + 32 * ft;
+    const float* sl = slope + size_t(n) * Fp + 32 * ft;
+    const size_t xr = size_t(n) * d * C;
+    const int second = two ? 32 : 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const int nn = n + (BF ? 8 * h + k : 2 * k + h);
-      const bool on = nn < n1;
-      const size_t at = size_t(on ? nn : n0);
+      const int o = min(8 * h + k, n1 - 1 - n);
+      const uint32_t at = uint32_t(o) * Fp + l32, xo = uint32_t(o) * d * C + (in_c ? c : 0);
       if constexpr (BF)
-        s.ab[k] = on && c < C ? static_cast<const uint16_t*>(x)[at * d * C + c] : uint16_t(0);
+        s.ab[k] = (static_cast<const uint16_t*>(x) + xr)[xo];
       else
-        s.a[k] = on && c < C ? static_cast<const float*>(x)[at * d * C + c] : 0.f;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const size_t i = at * Fp + 32 * (ft + j) + l32;
-        s.b[j][k] = on && (j == 0 || two) ? row_sum[i] : 0.f;
-        s.c[j][k] = on && (j == 0 || two) ? slope[i] : 0.f;
-      }
+        s.a[k] = (static_cast<const float*>(x) + xr)[xo];
+      s.b[0][k] = rs[at];
+      s.c[0][k] = sl[at];
+      s.b[1][k] = (rs + second)[at];
+      s.c[1][k] = (sl + second)[at];
     }
   };
   Step cur, nxt;
   load(n0, cur);
   for (int n = n0; n < n1; n += 16) {
     if (n + 16 < n1) load(n + 16, nxt);
+    u32x4 av[3];
+    float dq[2][8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) cur.b[j][k] *= cur.c[j][k];
-    if constexpr (BF) {
-      u32x4 av;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) av[k] = uint32_t(cur.ab[2 * k]) | uint32_t(cur.ab[2 * k + 1]) << 16;
+    for (int k = 0; k < 8; ++k) {
+      const bool on = n + 8 * h + k < n1;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float rest[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) rest[k] = cur.b[j][k];
-#pragma unroll
-        for (int part = 0; part < 3; ++part) {
-          u32x4 bv;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            bv[k] = pack_bf16x2_rne(rest[2 * k], rest[2 * k + 1]);
-            rest[2 * k] -= __uint_as_float(bv[k] << 16);
-            rest[2 * k + 1] -= __uint_as_float(bv[k] & 0xffff0000u);
-          }
-          acc[j] = mm<true>(av, bv, acc[j]);
-        }
+        dq[j][k] = on ? cur.b[j][k] * cur.c[j][k] : 0.f;
+        sum[j] += dq[j][k];
       }
+      if constexpr (BF)
+        cur.ab[k] = on && in_c ? cur.ab[k] : uint16_t(0);
+      else
+        cur.a[k] = on && in_c ? cur.a[k] : 0.f;
+    }
+    if constexpr (BF) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) av[0][k] = uint32_t(cur.ab[2 * k]) | uint32_t(cur.ab[2 * k + 1]) << 16;
     } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[j] = mfma32(cur.a[k], cur.b[j][k], acc[j]);
+      bf16_parts(cur.a, av);
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+      u32x4 bv[3];
+      bf16_parts(dq[j], bv);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum[j] += cur.b[j][k];
+      for (int order = 2; order >= 0; --order)  // the small products first
+#pragma unroll
+        for (int p = 0; p <= (BF ? 0 : order); ++p) acc[j] = mm<true>(av[p], bv[order - p], acc[j]);
+    }
     cur = nxt;
   }
 #pragma unroll
@@ -1140,10 +1187,16 @@ __global__ __launch_bounds__(256) void k_ffn_wsum(int C, int F, int FT, int S, i
 size_t al256(size_t b) { return (b + 255) & ~size_t(255); }
 
 struct Layout {
-  size_t pack[5], exps, s, ds, sum, r0, part, part_g, total;
-  int CT, FT, P, S, Sg, KS;
+  size_t pack[5], exps, s, ds, sum, r0, part, part_g, rows, total;
+  int CT, FT, P, S, Sg, KS, RS;
   size_t pack_bytes;
 };
+// Shares of the tiles of F in k_ffn_rows: enough workgroups for the device,
+// four tiles a share at least.
+int rows_shares(int M, int FT) {
+  const int wgs = (M + 127) / 128, shares = device_cus() / (wgs > 0 ? wgs : 1);
+  return std::max(1, std::min({shares, FT / 4, 8}));
+}
 // packs: up, down, gate (forward); W_up and W_down^T as up, W_up^T as down,
 // gate, W_gate^T as down (backward)
 Layout layout(const FfnShape& p, bool backward) {
@@ -1186,6 +1239,9 @@ Layout layout(const FfnShape& p, bool backward) {
     l.part_g = o;
     o += al256(size_t(l.Sg) * (p.C + 1) * 32 * l.FT * 4);
   }
+  l.RS = rows_shares(p.N * p.d, l.FT);
+  l.rows = o;
+  o += l.RS > 1 ? al256(size_t(l.RS) * p.N * p.d * p.C * 4) : 0;
   l.total = o;
   return l;
 }
@@ -1223,19 +1279,22 @@ hipError_t gate(const Layout& l, const FfnShape& p, const void* x, char* ws, int
 }
 
 template <int CT, bool BF, int NB>
-hipError_t rows_nb(const RowsArgs& a, hipStream_t s) {
+hipError_t rows_nb(const RowsArgs& a, int n_part, hipStream_t s) {
   const size_t lds = size_t(2) * 4 * CT * (BF ? 1 : 2) * kBlk * 16;
   auto k = k_ffn_rows<CT, BF, NB>;
   const hipError_t e =
       hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (e != hipSuccess) return e;
-  k<<<dim3((a.M + 128 * NB - 1) / (128 * NB)), dim3(256), lds, s>>>(a);
+  k<<<dim3((a.M + 128 * NB - 1) / (128 * NB), n_part), dim3(256), lds, s>>>(a);
+  const hipError_t e2 = hipGetLastError();
+  if (e2 != hipSuccess || n_part == 1) return e2;
+  k_ffn_join<BF><<<dim3(uint32_t((size_t(a.M) * a.C / 4 + 255) / 256)), dim3(256), 0, s>>>(a, n_part);
   return hipGetLastError();
 }
 
 template <int CT, bool BF>
-hipError_t rows(const RowsArgs& a, hipStream_t s) {
-  return rows_nb<CT, BF, 1>(a, s);
+hipError_t rows(const RowsArgs& a, int n_part, hipStream_t s) {
+  return rows_nb<CT, BF, 1>(a, n_part, s);
 }
 
 template <int CT, bool BF>
@@ -1263,7 +1322,8 @@ hipError_t forward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   r.s = reinterpret_cast<const float*>(ws + l.s);
   r.residual = a.residual;
   r.out = a.y;
-  return rows<CT, BF>(r, s);
+  r.partial = reinterpret_cast<float*>(ws + l.rows);
+  return rows<CT, BF>(r, l.RS, s);
 }
 
 template <int CT, bool BF>
@@ -1346,7 +1406,8 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   r.residual0 = r0;
   r.n_res0 = l.KS;
   r.out = a.grad_x;
-  return rows<CT, BF>(r, s);
+  r.partial = reinterpret_cast<float*>(ws + l.rows);
+  return rows<CT, BF>(r, l.RS, s);
 }
 
 template <bool BF>
