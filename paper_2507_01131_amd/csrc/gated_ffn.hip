@@ -41,6 +41,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlk = 64;  // u32x4 words of an operand block: 64 lanes x 8 values of 16 bits
 constexpr int kMaxFfnTiles = 128;  // F <= 4096
+// Row stride of the [.., F] arrays in the workspace: tiles of F made odd, so that
+// a column's rows do not fall on one memory channel (8192 nodes at F = 1024:
+// the gate 57 us at a stride of 4096 bytes).
+__host__ __device__ constexpr int ffn_stride(int FT) { return 32 * (FT | 1); }
 constexpr int kUnset = -1000;  // exponent of a sum that holds nothing yet
 
 template <bool BF>
@@ -305,10 +309,9 @@ __device__ __forceinline__ void lds_loads_done() {
   __syncthreads();
 }
 
-// s = act(q) and, if asked for, act'(q), [N, 32 FT] fp32 each: a workgroup
-// takes 128 nodes (lanes) and two tiles of hidden units.
-constexpr int kGateTiles = 2;
-template <int CT, bool BF>
+// s = act(q) and, if asked for, act'(q), [N, ffn_stride(FT)] fp32 each: a workgroup
+// takes 128 nodes (lanes) and kGateTiles tiles of hidden units.
+template <int CT, bool BF, int kGateTiles>
 __global__ __launch_bounds__(256) void k_ffn_gate(int N, int d, int C, int F, int FT, int act,
                                                   const void* __restrict__ x, const u32x4* __restrict__ wg,
                                                   const int* __restrict__ eg, const float* __restrict__ b,
@@ -363,8 +366,8 @@ __global__ __launch_bounds__(256) void k_ffn_gate(int N, int d, int C, int F, in
         dv[i] = f < F ? d1 : 0.f;
       }
       if (n < N) {
-        *reinterpret_cast<f32x4*>(s + size_t(n) * 32 * FT + f) = sv;
-        if (ds) *reinterpret_cast<f32x4*>(ds + size_t(n) * 32 * FT + f) = dv;
+        *reinterpret_cast<f32x4*>(s + size_t(n) * ffn_stride(FT) + f) = sv;
+        if (ds) *reinterpret_cast<f32x4*>(ds + size_t(n) * ffn_stride(FT) + f) = dv;
       }
     }
   }
@@ -376,7 +379,7 @@ struct RowsArgs {
   const void* in;            // [M, C]
   const u32x4 *up, *down;    // packed weights
   const int *e_up, *e_down;  // their exponents (fp32 problems)
-  const float* s;            // [M / d, 32 FT]
+  const float* s;            // [M / d, ffn_stride(FT)]
   const void* residual;      // [M, C] of the problem's type, or nullptr
   const float* residual0;    // [n_res0, M / d, C], added to the degree-0 rows, or nullptr
   int n_res0;
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
   __shared__ int s_bias[kMaxFfnTiles];                    // the tiles' exponents, of both weights
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int C = a.C, Fp = 32 * a.FT;
+  const int C = a.C, Fp = ffn_stride(a.FT);
   const int f0 = blockIdx.y * a.FT / gridDim.y, f1 = (blockIdx.y + 1) * a.FT / gridDim.y;
   auto fetch = [&](const u32x4* packed, int ft, int buf) {
     const u32x4* src = packed + size_t(ft) * kHalf;
@@ -575,8 +578,8 @@ __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const flo
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = (blockIdx.x * 4 + wave) * kTile + l32;
   const int f0 = blockIdx.y * FT / gridDim.y, f1 = (blockIdx.y + 1) * FT / gridDim.y;
-  const float* q = sum + size_t(min(n, N - 1)) * 32 * FT + 4 * h;
-  const float* ds = slope + size_t(min(n, N - 1)) * 32 * FT + 4 * h;
+  const float* q = sum + size_t(min(n, N - 1)) * ffn_stride(FT) + 4 * h;
+  const float* ds = slope + size_t(min(n, N - 1)) * ffn_stride(FT) + 4 * h;
   auto fetch = [&](int ft, int buf) {
     const u32x4* src = wg + size_t(ft) * kHalf;
     u32x4* dst = sw + buf * kHalf;
@@ -653,7 +656,7 @@ __device__ __forceinline__ void bf16_parts(float (&v)[8], u32x4 (&op)[3]) {
 // .. 8 h + 7) with the next step's loads in flight; 32x32x16 bf16 MFMA over
 // the bf16 parts of dq and of fp32 features, the products down to 2^-16 of the
 // first (six for fp32, three for bf16).  The waves of the first channel tile
-// also sum dq (grad b).  partial [S][C + 1][32 FT]: the last row is grad b.
+// also sum dq (grad b).  partial [S][C + 1][ffn_stride(FT)]: the last row is grad b.
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, int FT, const void* __restrict__ x,
                                                  const float* __restrict__ row_sum, const float* __restrict__ slope,
@@ -662,7 +665,7 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int FP = (FT + 1) / 2, t = blockIdx.x * 4 + wave;
   if (t >= CT * FP) return;
-  const int ct = t / FP, ft = 2 * (t - ct * FP), c = 32 * ct + l32, Fp = 32 * FT;
+  const int ct = t / FP, ft = 2 * (t - ct * FP), c = 32 * ct + l32, Fp = ffn_stride(FT);
   const int n0 = int(int64_t(blockIdx.y) * N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * N / gridDim.y);
   const bool two = ft + 1 < FT, in_c = c < C;
   f32x16 acc[2] = {f32x16{}, f32x16{}};
@@ -748,9 +751,9 @@ struct WgradArgs {
   const void *x, *gy;             // [N d, C]
   const u32x4 *up_u, *up_d;       // W_up and W_down^T packed as `up`
   const int *e_u, *e_d;
-  const float* s;                 // act(q) [N, 32 FT]
-  float* sum;                     // [N, 32 FT]: sum over a node's rows of dh u
-  float* partial;                 // [gridDim.y][2][C][32 FT]: W_down's (as [c][f]), then W_up's
+  const float* s;                 // act(q) [N, ffn_stride(FT)]
+  float* sum;                     // [N, ffn_stride(FT)]: sum over a node's rows of dh u
+  float* partial;                 // [gridDim.y][2][C][ffn_stride(FT)]: W_down's (as [c][f]), then W_up's
 };
 
 // Eight waves, two a SIMD: a wave's packed weights and sums fit 256 registers
@@ -815,7 +818,7 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // role 0: u and grad W_down; 1: dh and grad W_up
   const int hf = kHalves ? wave & 1 : 0, role = (kHalves ? wave >> 1 : wave) & 1, g = wave / (kHalves ? 4 : 2);
-  const int C = a.C, d = a.d, FT = a.FT, Fp = 32 * FT;
+  const int C = a.C, d = a.d, FT = a.FT, Fp = ffn_stride(FT);
   const int n0 = int(int64_t(blockIdx.y) * a.N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * a.N / gridDim.y);
   const int r0 = n0 * d, r1 = n1 * d;
   // waves without a tile of their own repeat the last one and store nothing
@@ -1151,7 +1154,7 @@ __global__ __launch_bounds__(256) void k_ffn_wsum(int C, int F, int FT, int S, i
                                                   void* __restrict__ gu, void* __restrict__ gg,
                                                   float* __restrict__ gb) {
   __shared__ float red[8][5][32];
-  const int Fp = 32 * FT, c0 = 4 * blockIdx.y, z = blockIdx.z;
+  const int Fp = ffn_stride(FT), c0 = 4 * blockIdx.y, z = blockIdx.z;
   const int col = threadIdx.x & 31, k = threadIdx.x >> 5, f = 32 * blockIdx.x + col;
   void* out = z == 0 ? gd : (z == 1 ? gu : gg);
   const bool bias = z == 2 && gb && blockIdx.y == 0;
@@ -1212,7 +1215,7 @@ Layout layout(const FfnShape& p, bool backward) {
   }
   l.exps = o;
   o += al256(size_t(5) * l.FT * 4);
-  const size_t gate = al256(size_t(p.N) * 32 * l.FT * 4);
+  const size_t gate = al256(size_t(p.N) * ffn_stride(l.FT) * 4);
   l.s = o;
   o += gate;
   if (backward) {
@@ -1230,14 +1233,14 @@ Layout layout(const FfnShape& p, bool backward) {
     l.S = p.N < most ? p.N : (most > 1 ? most : 1);
     if (l.S < 1) l.S = 1;
     l.part = o;
-    o += al256(size_t(l.S) * 2 * p.C * 32 * l.FT * 4);
+    o += al256(size_t(l.S) * 2 * p.C * ffn_stride(l.FT) * 4);
     const int blocks = (l.CT * ((l.FT + 1) / 2) + 3) / 4;
     int sg = 2 * device_cus() / blocks;
     const int cap = (p.N + 63) / 64;  // at least 64 nodes a range
     l.Sg = sg < cap ? sg : cap;
     if (l.Sg < 1) l.Sg = 1;
     l.part_g = o;
-    o += al256(size_t(l.Sg) * (p.C + 1) * 32 * l.FT * 4);
+    o += al256(size_t(l.Sg) * (p.C + 1) * ffn_stride(l.FT) * 4);
   }
   l.RS = rows_shares(p.N * p.d, l.FT);
   l.rows = o;
@@ -1263,19 +1266,29 @@ hipError_t pack(const PackArgs& a, const Layout& l, const FfnShape& p, hipStream
   return hipGetLastError();
 }
 
+template <int CT, bool BF, int T>
+hipError_t gate_t(const Layout& l, const FfnShape& p, const void* x, char* ws, int slot, const float* b, bool slope,
+                  hipStream_t s) {
+  const dim3 grid((p.N + 127) / 128, (l.FT + T - 1) / T);
+  constexpr int lds = T * 2 * CT * (BF ? 1 : 2) * kBlk * 16;
+  auto k = k_ffn_gate<CT, BF, T>;
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  k<<<grid, dim3(256), lds, s>>>(p.N, p.d, p.C, p.F, l.FT, p.act, x, reinterpret_cast<const u32x4*>(ws + l.pack[slot]),
+                                 reinterpret_cast<const int*>(ws + l.exps) + slot * l.FT, b,
+                                 reinterpret_cast<float*>(ws + l.s),
+                                 slope ? reinterpret_cast<float*>(ws + l.ds) : nullptr);
+  return hipGetLastError();
+}
+// Two tiles a workgroup read the features half as often (8192 x 256 -> 1024: 361
+// against 372 us for the backward); one where two would leave CUs idle (957 x
+// 16 x 80 -> 240: 80 against 74 us).
 template <int CT, bool BF>
 hipError_t gate(const Layout& l, const FfnShape& p, const void* x, char* ws, int slot, const float* b, bool slope,
                 hipStream_t s) {
-  const dim3 grid((p.N + 127) / 128, (l.FT + kGateTiles - 1) / kGateTiles);
-  constexpr int lds = kGateTiles * 2 * CT * (BF ? 1 : 2) * kBlk * 16;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_ffn_gate<CT, BF>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return e;
-  k_ffn_gate<CT, BF><<<grid, dim3(256), lds, s>>>(
-      p.N, p.d, p.C, p.F, l.FT, p.act, x, reinterpret_cast<const u32x4*>(ws + l.pack[slot]),
-      reinterpret_cast<const int*>(ws + l.exps) + slot * l.FT, b, reinterpret_cast<float*>(ws + l.s),
-      slope ? reinterpret_cast<float*>(ws + l.ds) : nullptr);
-  return hipGetLastError();
+  const bool two = int64_t((p.N + 127) / 128) * ((l.FT + 1) / 2) >= 2 * device_cus();
+  return two ? gate_t<CT, BF, 2>(l, p, x, ws, slot, b, slope, s) : gate_t<CT, BF, 1>(l, p, x, ws, slot, b, slope, s);
 }
 
 template <int CT, bool BF, int NB>
