@@ -1,0 +1,291 @@
+// The contraction of the attention block's backward (attention_bwd.hip): dg_e
+// and dalpha_e from x and Gz, instantiated per degree.
+#pragma once
+
+#include "common.hpp"
+#include "kernels.h"
+
+namespace tdn {
+namespace att_bwd_detail {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kBufferWord3 = 0x00020000;  // raw buffer resource, fourth word (gfx9 family)
+
+__device__ __forceinline__ f32x16 mfma_f16(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                0);
+}
+
+struct DgArgs {
+  int E, C, R, RT, H, n_range;
+  const int32_t *perm, *src, *dst;
+  const u32x4 *xp, *gp;            // x and Gz in launch_feature_layout_packed's words
+  const float *x_scale, *g_scale;  // their row scales
+  const u32x4* ops;                // k_att_factors
+  const float* f_scale;
+  const float* g;                  // [E, R] by sorted position
+  const float* alpha;              // [E, H] by sorted position
+  float* dg;                       // [E, R]
+  float* dal;                      // [E, H]
+};
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true);
+  return v + __builtin_bit_cast(float, o);
+}
+// sum over the 32 lanes of a lane's half, in every lane of it
+__device__ __forceinline__ float half_sum(float v) {
+  v = dpp_add<0xB1>(v);   // quad_perm [1, 0, 3, 2]
+  v = dpp_add<0x4E>(v);   // quad_perm [2, 3, 0, 1]
+  v = dpp_add<0x141>(v);  // mirrored within 8 lanes
+  v = dpp_add<0x140>(v);  // mirrored within 16 lanes
+  const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+// lanes 0 .. 31: the sum of a over the lane and its other half; lanes 32 .. 63: of b
+__device__ __forceinline__ float halves_of_two(float a, float b) {
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+__device__ __forceinline__ float both_halves(float v) { return halves_of_two(v, v); }
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+
+// waves a SIMD that the registers allow
+__host__ __device__ constexpr int dg_waves(int CT) { return CT <= 2 ? 3 : 2; }
+
+// sixteen-byte words of a slot: a node's, in whole direct loads of a wave
+__host__ __device__ constexpr int dg_slot(int ct_n, int n) { return (ct_n * 16 * n + kWave - 1) / kWave * kWave; }
+
+// A workgroup takes one range of sorted edges, a wave one tile of 32 ranks.
+// The range is a stream of items, x[s_e] of every edge and, before the first
+// edge of each destination, Gz[t]: one node's packed words each, brought into
+// one of two LDS slots by direct loads while the item before is worked on, so
+// that each item is read from L2 once for all ranks.  Bound by the matrix
+// instructions and, beside them, the sums of U V.
+template <int L, int CT, int PH>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(dg_waves(CT)))) void k_att_dg(DgArgs a) {
+  constexpr int d = (L + 1) * (L + 1), n = pk_rows(d), nb = pk_blocks(d), n4 = n / 4, nt = n % 4;
+  constexpr int H = CT / PH;
+  extern __shared__ u32x4 smem[];  // two slots of a node's words, [RT][64][H] of dalpha's shares, alpha
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int rt = __builtin_amdgcn_readfirstlane(tid >> 6);  // the wave's rank tile
+  const int RT = a.RT, R = a.R, threads = RT * kWave;
+  const int range = xcd_remap(blockIdx.x, gridDim.x);
+  const int e0 = int(int64_t(range) * a.E / a.n_range), e1 = int(int64_t(range + 1) * a.E / a.n_range);
+  if (e0 >= e1) return;  // (the whole workgroup)
+  constexpr int words4 = CT * 16 * n, slot4 = dg_slot(CT, n);  // a node's words, sixteen bytes each
+  float* s_dal = reinterpret_cast<float*>(smem + 2 * slot4);
+  float* s_al = s_dal + RT * kWave * H;  // alpha of the batch [64][H]
+  const int r = rt * kTile + l32;
+  const float un = a.f_scale[r] * a.f_scale[RT * kTile + r];
+  u32x4 Aop[nb];
+#pragma unroll
+  for (int b = 0; b < nb; ++b) Aop[b] = a.ops[(size_t(b) * RT + rt) * kWave + lane];
+  const u32x4* Dop = a.ops + (size_t(nb) * RT + rt) * kWave + lane;
+  // records of 64 sorted edges, one a lane, and of the 64 after them
+  struct Rec {
+    int src, dst;
+    float sc;
+  };
+  auto load_batch = [&](int b0) {
+    Rec rec{0, -1, 1.f};
+    if (b0 + lane < e1) {
+      const int eid = a.perm[b0 + lane];
+      rec.src = a.src[eid];
+      rec.dst = a.dst[eid];
+      rec.sc = a.x_scale[rec.src] * a.g_scale[rec.dst];
+    }
+    return rec;
+  };
+  auto load_alpha = [&](int b0) {
+    for (int i = tid; i < min(kWave, e1 - b0) * H; i += threads) s_al[i] = a.alpha[size_t(b0) * H + i];
+  };
+  Rec cur = load_batch(e0), nxt = load_batch(e0 + kWave);
+  int b0 = e0;
+  auto of = [&](int in_cur, int in_nxt, int e) {
+    const int i = e - b0;
+    return i < kWave ? __builtin_amdgcn_readlane(in_cur, i) : __builtin_amdgcn_readlane(in_nxt, i - kWave);
+  };
+  auto src_of = [&](int e) { return of(cur.src, nxt.src, e); };
+  auto dst_of = [&](int e) { return of(cur.dst, nxt.dst, e); };
+  // (lanes behind the node's words read zeros through the range check, into
+  // the slot's padding)
+  auto fetch = [&](const u32x4* base, int node, int slot) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<u32x4*>(base) + size_t(node) * words4, 0, words4 * 16, kBufferWord3);
+    u32x4* dst = smem + slot * slot4;
+    for (int i = rt * kWave; i < words4; i += threads)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(dst + i), 16, lane * 16,
+                                               i * 16, 0, 0);
+  };
+  // channel tile ct of the item in a slot, as the K blocks of a contraction
+  auto load_words = [&](const u32x4* slot, int ct, uint32_t (&w)[n]) {
+    const u32x4* p = slot + ct * 16 * n;
+#pragma unroll
+    for (int q = 0; q < n4; ++q) {
+      const u32x4 v = p[q * kWave + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[4 * q + i] = v[i];
+    }
+    const uint32_t* t = reinterpret_cast<const uint32_t*>(p + n4 * kWave) + nt * lane;
+#pragma unroll
+    for (int i = 0; i < nt; ++i) w[4 * n4 + i] = t[i];
+  };
+  auto block = [&](const uint32_t (&w)[n], int b) {
+    u32x4 v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = w[4 * b + k < n ? 4 * b + k : 4 * b + k - n];
+    return v;
+  };
+  auto item_ready = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share is in LDS
+    __syncthreads();                     // every wave's is, and the other slot is free
+  };
+  f32x16 U[CT];
+  load_alpha(e0);  // (read behind the next barrier)
+  fetch(a.gp, dst_of(e0), 0);
+  int slot = 0, t_cur = -1;
+  float g_next = r < R ? a.g[size_t(e0) * R + r] : 0.f;
+  for (int e = e0; e < e1; ++e) {
+    const int j = e - b0;
+    const int t = __builtin_amdgcn_readlane(cur.dst, j);
+    if (t != t_cur) {  // Gz[t] is in the slot: U_t, while x[s_e] comes
+      t_cur = t;
+      item_ready();
+      fetch(a.xp, __builtin_amdgcn_readlane(cur.src, j), slot ^ 1);
+      u32x4 Dv[nb];
+#pragma unroll
+      for (int b = 0; b < nb; ++b) Dv[b] = Dop[size_t(b) * RT * kWave];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        uint32_t w[n];
+        load_words(smem + slot * slot4, ct, w);
+        U[ct] = f32x16{};
+#pragma unroll
+        for (int b = 0; b < nb; ++b) U[ct] = mfma_f16(block(w, b), Dv[b], U[ct]);
+      }
+      slot ^= 1;
+    }
+    item_ready();
+    const float ge = g_next;
+    if (e + 1 < e1) {
+      const int tn = dst_of(e + 1);
+      fetch(tn != t ? a.gp : a.xp, tn != t ? tn : src_of(e + 1), slot ^ 1);
+      g_next = r < R ? a.g[size_t(e + 1) * R + r] : 0.f;
+    }
+    const float sc = lane_value(cur.sc, j) * un;
+    // V of a channel tile beside the sums of U V of the tile before
+    float p[H];
+#pragma unroll
+    for (int k = 0; k < H; ++k) p[k] = 0.f;
+    uint32_t w[2][n];
+    load_words(smem + slot * slot4, 0, w[0]);
+    f32x16 V[2];
+#pragma unroll
+    for (int ct = 0; ct <= CT; ++ct) {
+      if (ct + 1 < CT) load_words(smem + slot * slot4, ct + 1, w[(ct + 1) & 1]);
+      float q[4] = {0.f, 0.f, 0.f, 0.f};
+      if (ct < CT) V[ct & 1] = f32x16{};
+#pragma unroll
+      for (int b = 0; b < nb; ++b) {
+        if (ct < CT) V[ct & 1] = mfma_f16(block(w[ct & 1], b), Aop[b], V[ct & 1]);
+        if (ct > 0)
+#pragma unroll
+          for (int v = b * 16 / nb; v < (b + 1) * 16 / nb; ++v)
+            q[v & 3] = fmaf(U[ct > 0 ? ct - 1 : 0][v], V[(ct + 1) & 1][v], q[v & 3]);
+      }
+      if (ct > 0) p[(ct - 1) / PH] += (q[0] + q[1]) + (q[2] + q[3]);
+    }
+    slot ^= 1;
+    // heads in pairs: one's sums over channels in lanes 0 .. 31, the other's
+    // in lanes 32 .. 63
+    float dge = 0.f;
+#pragma unroll
+    for (int k = 0; k < H; k += 2) {
+      const bool on = k + 1 < H || h == 0;
+      const int kh = k + 1 < H ? k + h : k;
+      const float al = on ? s_al[j * H + kh] : 0.f;
+      const float P = halves_of_two(p[k], k + 1 < H ? p[k + 1 < H ? k + 1 : k] : 0.f) * sc;
+      dge = fmaf(al, P, dge);
+      const float da = half_sum(P * ge);
+      if (l32 == 0 && on) s_dal[(rt * kWave + j) * H + kh] = da;
+    }
+    dge = both_halves(dge);
+    if (h == 0 && r < R) a.dg[size_t(e) * R + r] = dge;
+    if (j + 1 == kWave || e + 1 == e1) {
+      // dalpha of the batch: the rank tiles' shares in order
+      __syncthreads();
+      for (int i = tid; i < (j + 1) * H; i += threads) {
+        float v = 0.f;
+        for (int q = 0; q < RT; ++q) v += s_dal[q * kWave * H + i];
+        a.dal[size_t(b0) * H + i] = v;
+      }
+      __syncthreads();
+      cur = nxt;
+      b0 += kWave;
+      nxt = load_batch(b0 + kWave);
+      load_alpha(b0);
+    }
+  }
+}
+
+// LDS: two nodes' words, then a batch's shares of dalpha and its alpha
+inline int dg_lds(const DgArgs& a, int d) {
+  return 2 * 16 * dg_slot(a.C / kTile, pk_rows(d)) + (a.RT + 1) * kWave * a.H * 4;
+}
+
+template <int L, int CT, int PH>
+hipError_t launch_dg_k(DgArgs& g, hipStream_t s) {
+  const int lds = dg_lds(g, (L + 1) * (L + 1));
+  auto k = k_att_dg<L, CT, PH>;
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  // as many workgroups as the device holds
+  const int by_lds = 160 * 1024 / lds, by_waves = 4 * dg_waves(CT) / g.RT;
+  const int per_cu = by_lds < by_waves ? by_lds : by_waves;
+  const int ranges = device_cus() * (per_cu < 1 ? 1 : per_cu);
+  g.n_range = ranges < g.E ? ranges : g.E;
+  k<<<dim3(g.n_range), dim3(g.RT * kWave), lds, s>>>(g);
+  return hipGetLastError();
+}
+
+// C / 32 channel tiles, tiles per head (a divisor)
+template <int L>
+hipError_t launch_dg_l(DgArgs& g, hipStream_t s) {
+  const int ct = g.C / kTile, ph = ct / g.H;
+  switch (ct * 16 + ph) {
+#define TDN_DG_CASE(CTV, PHV) \
+  case CTV * 16 + PHV: return launch_dg_k<L, CTV, PHV>(g, s);
+    TDN_DG_CASE(1, 1)
+    TDN_DG_CASE(2, 1)
+    TDN_DG_CASE(2, 2)
+    TDN_DG_CASE(3, 1)
+    TDN_DG_CASE(3, 3)
+    TDN_DG_CASE(4, 1)
+    TDN_DG_CASE(4, 2)
+    TDN_DG_CASE(4, 4)
+    TDN_DG_CASE(5, 1)
+    TDN_DG_CASE(5, 5)
+    TDN_DG_CASE(6, 1)
+    TDN_DG_CASE(6, 2)
+    TDN_DG_CASE(6, 3)
+    TDN_DG_CASE(6, 6)
+    TDN_DG_CASE(7, 1)
+    TDN_DG_CASE(7, 7)
+    TDN_DG_CASE(8, 1)
+    TDN_DG_CASE(8, 2)
+    TDN_DG_CASE(8, 4)
+    TDN_DG_CASE(8, 8)
+#undef TDN_DG_CASE
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace att_bwd_detail
+}  // namespace tdn
