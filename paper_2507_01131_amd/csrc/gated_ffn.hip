@@ -382,186 +382,142 @@ struct RowsArgs {
   const float* s;            // [M / d, ffn_stride(FT)]
   const void* residual;      // [M, C] of the problem's type, or nullptr
   const float* residual0;    // [n_res0, M / d, C], added to the degree-0 rows, or nullptr
-  int n_res0;
+  int n_res0;                // (one in k_ffn_rows, any number in k_ffn_join)
   void* out;                 // [M, C]
-  float* partial;            // [gridDim.y, M, C] where the tiles of F are shared out (gridDim.y > 1)
+  // row tiles of 128 rows: the first `full` with all tiles of F to a workgroup,
+  // the `rem` behind them with shares of F to a workgroup
+  int full, rem, shares;
+  float* partial;  // [shares, M - 128 full, C] where shares > 1
 };
 
-// Waves a SIMD: two where a wave's rows and sums leave room in 256 registers.
-__host__ __device__ constexpr int rows_waves(int CT, bool BF, int NB) {
-  return NB * CT * (BF ? 24 : 32) <= (BF ? 168 : 128) ? 2 : 1;
-}
+// Waves a SIMD: two where a wave's rows and sums leave room in 256 registers
+// (fp32, C = 160: 146 us with one, 135 with two at 80000 rows, F = 512; C = 128:
+// 134 and 99; bf16, C = 256, 102400 rows, F = 1024: 200 and 178).
+__host__ __device__ constexpr int rows_waves(int CT, bool BF) { return CT <= (BF ? 8 : 5) ? 2 : 1; }
 
-// A workgroup takes 4 x 32 NB rows.  The packed weights come into LDS by
-// direct loads one tile of F ahead of their use, and u of the next tile is
-// formed beside the conversion of this tile's h, so that neither the loads
-// nor the vector work stand between the matrix instructions.  With gridDim.y
-// > 1 the workgroups of one y take a share of the tiles, and k_ffn_join adds
-// their sums.
-template <int CT, bool BF, int NB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(CT, BF, NB)))) void k_ffn_rows(
-    RowsArgs a) {
+// A workgroup takes 4 x 32 rows; a wave keeps its rows x and its sums y in
+// registers.  The packed weights of the next tile of F come into LDS by direct
+// loads while this tile's are used.  Within a tile nothing is overlapped by
+// hand: a second wave on the SIMD fills the gaps, and a form that made the next
+// tile's u beside the conversion of h needed its registers (bf16, 102400 x 256 ->
+// 1024: 227 us with it, 178 without).  Bound by the LDS reads of the weights,
+// which every wave makes for its own 32 rows: as many cycles as the matrix
+// instructions.  Row tiles that would leave CUs idle have the tiles of F shared
+// out, and k_ffn_join adds the shares' sums.
+template <int CT, bool BF>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(CT, BF)))) void k_ffn_rows(RowsArgs a) {
   constexpr int P = BF ? 1 : 2;
   constexpr int kHalf = 2 * CT * P * kBlk;  // words of a tile's up (and down) operands
-  constexpr int kWaves = rows_waves(CT, BF, NB), kDepth = kWaves == 2 ? 3 : 4;
-  constexpr int kChains = kWaves == 2 || NB > 1 ? 1 : 2;  // of a row tile's u
-  extern __shared__ u32x4 sw[];                           // up [2][kHalf], down [2][kHalf]
-  __shared__ int s_bias[kMaxFfnTiles];                    // the tiles' exponents, of both weights
+  extern __shared__ u32x4 sw[];             // two tiles' up [kHalf] and down [kHalf]
+  __shared__ int s_bias[kMaxFfnTiles];      // the tiles' exponents, of both weights
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int C = a.C, Fp = ffn_stride(a.FT);
-  const int f0 = blockIdx.y * a.FT / gridDim.y, f1 = (blockIdx.y + 1) * a.FT / gridDim.y;
-  auto fetch = [&](const u32x4* packed, int ft, int buf) {
-    const u32x4* src = packed + size_t(ft) * kHalf;
-    u32x4* dst = sw + buf * kHalf;
-    blocks_to_lds<CT * P / 2>(src, dst, wave, lane);
-    if constexpr (CT * P % 2 == 1)  // an odd pair of blocks is left
-      if (wave < 2) blocks_to_lds<1>(src + 4 * (CT * P / 2) * kBlk, dst + 4 * (CT * P / 2) * kBlk, wave, lane);
+  int tile = blockIdx.x, share = 0, shares = 1;
+  if (tile >= a.full) {
+    shares = a.shares;
+    share = (tile - a.full) / a.rem;
+    tile -= share * a.rem;
+  }
+  const int f0 = share * a.FT / shares, f1 = (share + 1) * a.FT / shares;
+  auto fetch = [&](int ft, int buf) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const u32x4* src = (k ? a.down : a.up) + size_t(ft) * kHalf;
+      u32x4* dst = sw + (buf * 2 + k) * kHalf;
+      blocks_to_lds<CT * P / 2>(src, dst, wave, lane);
+      if constexpr (CT * P % 2 == 1)  // an odd pair of blocks is left
+        if (wave < 2) blocks_to_lds<1>(src + 4 * (CT * P / 2) * kBlk, dst + 4 * (CT * P / 2) * kBlk, wave, lane);
+    }
   };
-  // (buffers go by the parity of the tile's place in the share)
-  fetch(a.up, f0, 0);
-  if (f0 + 1 < f1) fetch(a.up, f0 + 1, 1);
-  fetch(a.down, f0, 2);
+  fetch(f0, 0);
   if constexpr (!BF)
     for (int i = f0 + threadIdx.x; i < f1; i += 256) s_bias[i] = a.e_up[i] + a.e_down[i];
-  int row[NB], ex[NB], E[NB];
-  const float* s[NB];
-  u32x4 xo[NB][2 * CT][P];
-  f32x16 y[NB][CT], u[NB];
-  f32x4 sv[NB][4];
+  const int row = (tile * 4 + wave) * kTile + l32;
+  const bool on = row < a.M;
+  const int r = on ? row : a.M - 1;
+  u32x4 xo[2 * CT][P];
+  const int ex = load_row<CT, BF>(a.in, on, size_t(r) * C, C, h, xo);
+  const float* s = a.s + size_t(r / a.d) * Fp + 4 * h;
+  int E = kUnset;
+  f32x16 y[CT];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    row[b] = (blockIdx.x * 4 + wave) * (kTile * NB) + b * kTile + l32;
-    const bool on = row[b] < a.M;
-    const int r = on ? row[b] : a.M - 1;
-    ex[b] = load_row<CT, BF>(a.in, on, size_t(r) * C, C, h, xo[b]);
-    s[b] = a.s + size_t(r / a.d) * Fp + 4 * h;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 32 * f0 + 8 * k);
-    E[b] = kUnset;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) y[b][ct] = f32x16{};
-  }
-  // u of one tile; beside(i) is the vector work that goes with step i
-  auto up_product = [&](int buf, auto beside) {
-    f32x16 c[NB][kChains];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int k = 0; k < kChains; ++k) c[b][k] = f32x16{};
-    stream_blocks<2 * CT, P, kDepth>(sw + buf * kHalf + lane, [&](int st, const u32x4* wa) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b) c[b][st % kChains] = mm_parts<BF>(wa, xo[b][st], c[b][st % kChains]);
-      beside(st);
-    });
-#pragma unroll
-    for (int b = 0; b < NB; ++b) u[b] = kChains == 2 ? c[b][0] + c[b][kChains - 1] : c[b][0];
-  };
-  lds_loads_done();
-  up_product(0, [](int) {});
+  for (int ct = 0; ct < CT; ++ct) y[ct] = f32x16{};
   for (int ft = f0; ft < f1; ++ft) {
     const int odd = (ft - f0) & 1;
-    lds_loads_done();  // W_up of tile ft + 1 and W_down of tile ft; the buffers used before are free
-    if (ft + 2 < f1) fetch(a.up, ft + 2, odd);
-    if (ft + 1 < f1) fetch(a.down, ft + 1, 2 + (odd ^ 1));
-    const int bias = BF ? 0 : s_bias[ft];
-    u32x4 ho[NB][2][P];
-    float t[NB][16], sc[NB];
+    lds_loads_done();  // the weights of tile ft; the buffers used before are free
+    f32x4 sv[4];       // (before the direct loads: loads come back in order)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
+    for (int k = 0; k < 4; ++k) sv[k] = *reinterpret_cast<const f32x4*>(s + 32 * ft + 8 * k);
+    if (ft + 1 < f1) fetch(ft + 1, odd ^ 1);
+    f32x16 u = f32x16{};
+    stream_blocks<2 * CT, P, 2>(sw + odd * 2 * kHalf + lane,
+                                [&](int st, const u32x4* wa) { u = mm_parts<BF>(wa, xo[st], u); });
+    float t[16];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) t[b][v] = u[b][v] * sv[b][v >> 2][v & 3];
-      sc[b] = operand_scale<BF>(t[b], bias, E[b], [&](float f) {
+    for (int v = 0; v < 16; ++v) t[v] = u[v] * sv[v >> 2][v & 3];
+    const float sc = operand_scale<BF>(t, BF ? 0 : s_bias[ft], E, [&](float f) {
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) y[b][ct] *= f;
-      });
-    }
-    // the pairs of h, spread over the steps of the next tile's u
-    auto convert = [&](int st) {
+      for (int ct = 0; ct < CT; ++ct) y[ct] *= f;
+    });
+    u32x4 ho[2][P];
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i * 2 * CT / 8 == st) operand_pair<BF>(t[b], sc[b], i, ho[b]);
-    };
-    if (ft + 1 < f1) {
-      up_product(odd ^ 1, convert);
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sv[b][k] = *reinterpret_cast<const f32x4*>(s[b] + 32 * (ft + 1) + 8 * k);
-    } else {
-#pragma unroll
-      for (int st = 0; st < 2 * CT; ++st) convert(st);
-    }
-    stream_blocks<2 * CT, P, kDepth>(sw + (2 + odd) * kHalf + lane, [&](int i, const u32x4* wa) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b) y[b][i >> 1] = mm_parts<BF>(wa, ho[b][i & 1], y[b][i >> 1]);
+    for (int i = 0; i < 8; ++i) operand_pair<BF>(t, sc, i, ho);
+    stream_blocks<2 * CT, P, 2>(sw + (odd * 2 + 1) * kHalf + lane, [&](int i, const u32x4* wa) {
+      y[i >> 1] = mm_parts<BF>(wa, ho[i & 1], y[i >> 1]);
     });
   }
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    if (row[b] >= a.M) continue;
-    const int e = BF ? 0 : E[b] + ex[b];
-    const int n = row[b] / a.d;
-    if constexpr (!BF)
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) y[b][ct][v] = ldexpf(y[b][ct][v], e);
-    if (gridDim.y > 1) {
-      float* out = a.partial + (size_t(blockIdx.y) * a.M + row[b]) * C + 4 * h;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (32 * ct + 8 * k + 4 * h < C)
-            *reinterpret_cast<f32x4*>(out + 32 * ct + 8 * k) =
-                f32x4{y[b][ct][4 * k], y[b][ct][4 * k + 1], y[b][ct][4 * k + 2], y[b][ct][4 * k + 3]};
-      continue;
-    }
-    if (a.residual0 && n * a.d == row[b])
-      for (int p = 0; p < a.n_res0; ++p) {
-        const float* r0 = a.residual0 + (size_t(p) * (a.M / a.d) + n) * C + 4 * h;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const f32x4 r = 32 * ct + 8 * k < C ? *reinterpret_cast<const f32x4*>(r0 + 32 * ct + 8 * k) : f32x4{};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[b][ct][4 * k + i] += r[i];
-          }
-      }
+  if (!on) return;
+  if constexpr (!BF)
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = 32 * ct + 8 * k + 4 * h;
-        if (c >= C) continue;
-        f32x4 v{y[b][ct][4 * k], y[b][ct][4 * k + 1], y[b][ct][4 * k + 2], y[b][ct][4 * k + 3]};
-        if (a.residual) v += load4<BF>(a.residual, size_t(row[b]) * C + c);
-        store4<BF>(a.out, size_t(row[b]) * C + c, v);
-      }
+      for (int v = 0; v < 16; ++v) y[ct][v] = ldexpf(y[ct][v], E + ex);
+  if (shares > 1) {
+    const size_t row0 = size_t(a.full) * 128;
+    float* out = a.partial + (share * (a.M - row0) + row - row0) * C + 4 * h;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (32 * ct + 8 * k + 4 * h < C)
+          *reinterpret_cast<f32x4*>(out + 32 * ct + 8 * k) =
+              f32x4{y[ct][4 * k], y[ct][4 * k + 1], y[ct][4 * k + 2], y[ct][4 * k + 3]};
+    return;
   }
+  const int n = row / a.d;
+  const float* r0 = a.residual0 && n * a.d == row ? a.residual0 + size_t(n) * C : nullptr;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = 32 * ct + 8 * k + 4 * h;
+      if (c >= C) continue;
+      f32x4 v{y[ct][4 * k], y[ct][4 * k + 1], y[ct][4 * k + 2], y[ct][4 * k + 3]};
+      if (r0) v += *reinterpret_cast<const f32x4*>(r0 + c);
+      if (a.residual) v += load4<BF>(a.residual, size_t(row) * C + c);
+      store4<BF>(a.out, size_t(row) * C + c, v);
+    }
 }
 
 // The shares' sums in order, with the residuals, four channels a thread.
 template <bool BF>
-__global__ __launch_bounds__(256) void k_ffn_join(RowsArgs a, int n_part) {
-  const size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * 4, total = size_t(a.M) * a.C;
+__global__ __launch_bounds__(256) void k_ffn_join(RowsArgs a) {
+  const size_t before = size_t(a.full) * 128 * a.C, total = size_t(a.M) * a.C - before;
+  const size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * 4, o = before + i;
   if (i >= total) return;
   f32x4 v = f32x4{};
 #pragma unroll 4
-  for (int p = 0; p < n_part; ++p) v += *reinterpret_cast<const f32x4*>(a.partial + p * total + i);
-  if (a.residual) v += load4<BF>(a.residual, i);
+  for (int p = 0; p < a.shares; ++p) v += *reinterpret_cast<const f32x4*>(a.partial + p * total + i);
+  if (a.residual) v += load4<BF>(a.residual, o);
   if (a.residual0) {
-    const int row = int(i / a.C), n = row / a.d;
-    const size_t c = i - size_t(row) * a.C;
+    const int row = int(o / a.C), n = row / a.d;
+    const size_t c = o - size_t(row) * a.C;
     if (n * a.d == row)
       for (int p = 0; p < a.n_res0; ++p)
         v += *reinterpret_cast<const f32x4*>(a.residual0 + (size_t(p) * (a.M / a.d) + n) * a.C + c);
   }
-  store4<BF>(a.out, i, v);
+  store4<BF>(a.out, o, v);
 }
 
 // ------------------------------------------------------ the gate's gradients
@@ -1191,14 +1147,20 @@ size_t al256(size_t b) { return (b + 255) & ~size_t(255); }
 
 struct Layout {
   size_t pack[5], exps, s, ds, sum, r0, part, part_g, rows, total;
-  int CT, FT, P, S, Sg, KS, RS;
+  int CT, FT, P, S, Sg, KS;
   size_t pack_bytes;
 };
-// Shares of the tiles of F in k_ffn_rows: enough workgroups for the device,
-// four tiles a share at least.
-int rows_shares(int M, int FT) {
-  const int wgs = (M + 127) / 128, shares = device_cus() / (wgs > 0 ? wgs : 1);
-  return std::max(1, std::min({shares, FT / 4, 8}));
+// The row tiles of k_ffn_rows: as many rounds of the device's workgroups as they
+// fill, then the tiles that are left, with F shared out over the device, four
+// tiles of F a share at least.
+struct RowsPlan {
+  int full, rem, shares;
+};
+RowsPlan rows_plan(int M, const Layout& l) {
+  const int tiles = (M + 127) / 128, slots = device_cus();
+  RowsPlan p{tiles / slots * slots, tiles % slots, 1};
+  if (p.rem > 0) p.shares = std::max(1, std::min({slots / p.rem, l.FT / 4, 8}));
+  return p;
 }
 // packs: up, down, gate (forward); W_up and W_down^T as up, W_up^T as down,
 // gate, W_gate^T as down (backward)
@@ -1242,9 +1204,9 @@ Layout layout(const FfnShape& p, bool backward) {
     l.part_g = o;
     o += al256(size_t(l.Sg) * (p.C + 1) * ffn_stride(l.FT) * 4);
   }
-  l.RS = rows_shares(p.N * p.d, l.FT);
+  const RowsPlan r = rows_plan(p.N * p.d, l);
   l.rows = o;
-  o += l.RS > 1 ? al256(size_t(l.RS) * p.N * p.d * p.C * 4) : 0;
+  if (r.shares > 1) o += al256(r.shares * (size_t(p.N) * p.d - size_t(r.full) * 128) * p.C * 4);
   l.total = o;
   return l;
 }
@@ -1291,23 +1253,39 @@ hipError_t gate(const Layout& l, const FfnShape& p, const void* x, char* ws, int
   return two ? gate_t<CT, BF, 2>(l, p, x, ws, slot, b, slope, s) : gate_t<CT, BF, 1>(l, p, x, ws, slot, b, slope, s);
 }
 
-template <int CT, bool BF, int NB>
-hipError_t rows_nb(const RowsArgs& a, int n_part, hipStream_t s) {
-  const size_t lds = size_t(2) * 4 * CT * (BF ? 1 : 2) * kBlk * 16;
-  auto k = k_ffn_rows<CT, BF, NB>;
-  const hipError_t e =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
-  if (e != hipSuccess) return e;
-  k<<<dim3((a.M + 128 * NB - 1) / (128 * NB), n_part), dim3(256), lds, s>>>(a);
-  const hipError_t e2 = hipGetLastError();
-  if (e2 != hipSuccess || n_part == 1) return e2;
-  k_ffn_join<BF><<<dim3(uint32_t((size_t(a.M) * a.C / 4 + 255) / 256)), dim3(256), 0, s>>>(a, n_part);
+template <bool BF>
+hipError_t join(const RowsArgs& a, hipStream_t s) {
+  const size_t left = (a.M - size_t(a.full) * 128) * a.C;
+  k_ffn_join<BF><<<dim3(uint32_t((left / 4 + 255) / 256)), dim3(256), 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <int CT, bool BF>
-hipError_t rows(const RowsArgs& a, int n_part, hipStream_t s) {
-  return rows_nb<CT, BF, 1>(a, n_part, s);
+hipError_t rows(RowsArgs& a, const Layout& l, hipStream_t s) {
+  const size_t lds = size_t(2) * 4 * CT * (BF ? 1 : 2) * kBlk * 16;
+  auto k = k_ffn_rows<CT, BF>;
+  hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+  if (e != hipSuccess) return e;
+  const RowsPlan p = rows_plan(a.M, l);
+  if (a.n_res0 > 1 && (p.full > 0 || p.shares == 1)) {  // k_ffn_rows adds them: their sum first, in place
+    RowsArgs j{};
+    j.M = a.M / a.d;
+    j.d = 1;
+    j.C = a.C;
+    j.shares = a.n_res0;
+    j.partial = const_cast<float*>(a.residual0);
+    j.out = j.partial;
+    e = join<false>(j, s);
+    if (e != hipSuccess) return e;
+    a.n_res0 = 1;
+  }
+  a.full = p.full;
+  a.rem = p.rem;
+  a.shares = p.shares;
+  k<<<dim3(p.full + p.rem * p.shares), dim3(256), lds, s>>>(a);
+  e = hipGetLastError();
+  return e != hipSuccess || p.shares == 1 ? e : join<BF>(a, s);
 }
 
 template <int CT, bool BF>
@@ -1336,7 +1314,7 @@ hipError_t forward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   r.residual = a.residual;
   r.out = a.y;
   r.partial = reinterpret_cast<float*>(ws + l.rows);
-  return rows<CT, BF>(r, l.RS, s);
+  return rows<CT, BF>(r, l, s);
 }
 
 template <int CT, bool BF>
@@ -1420,7 +1398,7 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   r.n_res0 = l.KS;
   r.out = a.grad_x;
   r.partial = reinterpret_cast<float*>(ws + l.rows);
-  return rows<CT, BF>(r, l.RS, s);
+  return rows<CT, BF>(r, l, s);
 }
 
 template <bool BF>
