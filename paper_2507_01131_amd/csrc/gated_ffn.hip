@@ -310,66 +310,66 @@ __device__ __forceinline__ void lds_loads_done() {
 }
 
 // s = act(q) and, if asked for, act'(q), [N, ffn_stride(FT)] fp32 each: a workgroup
-// takes 128 nodes (lanes) and kGateTiles tiles of hidden units.
-template <int CT, bool BF, int kGateTiles>
-__global__ __launch_bounds__(256) void k_ffn_gate(int N, int d, int C, int F, int FT, int act,
-                                                  const void* __restrict__ x, const u32x4* __restrict__ wg,
-                                                  const int* __restrict__ eg, const float* __restrict__ b,
-                                                  float* __restrict__ s, float* __restrict__ ds) {
+// takes 128 nodes (lanes) and a share of the tiles of hidden units, the next
+// tile's weights on their way to LDS while this one's are used.  Bound by the
+// writes of s and act'(q) and the reads of the weights.
+template <int CT, bool BF>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_ffn_gate(
+    int N, int d, int C, int F, int FT, int act, const void* __restrict__ x, const u32x4* __restrict__ wg,
+    const int* __restrict__ eg, const float* __restrict__ b, float* __restrict__ s, float* __restrict__ ds) {
   constexpr int P = BF ? 1 : 2, kHalf = 2 * CT * P * kBlk;
-  extern __shared__ u32x4 sw[];  // [kGateTiles][kHalf]
+  extern __shared__ u32x4 sw[];  // [2][kHalf]
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = (blockIdx.x * 4 + wave) * kTile + l32;
-  const int f0 = blockIdx.y * kGateTiles, tiles = min(kGateTiles, FT - f0);
-  if constexpr (CT * P % 2 == 0) {
-#pragma unroll
-    for (int t = 0; t < kGateTiles; ++t)
-      if (t < tiles)
-        blocks_to_lds<CT * P / 2>(wg + size_t(f0 + t) * kHalf, sw + t * kHalf, wave, lane);
-  } else {
-    for (int i = threadIdx.x; i < tiles * kHalf; i += 256) sw[i] = wg[size_t(f0) * kHalf + i];
-  }
+  const int f0 = blockIdx.y * FT / gridDim.y, f1 = (blockIdx.y + 1) * FT / gridDim.y;
+  auto fetch = [&](int ft, int buf) {
+    const u32x4* src = wg + size_t(ft) * kHalf;
+    u32x4* dst = sw + buf * kHalf;
+    blocks_to_lds<CT * P / 2>(src, dst, wave, lane);
+    if constexpr (CT * P % 2 == 1)  // an odd pair of blocks is left
+      if (wave < 2) blocks_to_lds<1>(src + 4 * (CT * P / 2) * kBlk, dst + 4 * (CT * P / 2) * kBlk, wave, lane);
+  };
+  fetch(f0, 0);
   u32x4 xo[2 * CT][P];
   const int ex = load_row<CT, BF>(x, n < N, n < N ? size_t(n) * d * C : 0, C, h, xo);
-  f32x4 bias[kGateTiles][4];
-#pragma unroll
-  for (int t = 0; t < kGateTiles; ++t)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int f = 32 * (f0 + t) + 8 * k + 4 * h;  // (F is a multiple of 16: a quad is inside or outside)
-      bias[t][k] = b && f < F ? *reinterpret_cast<const f32x4*>(b + f) : f32x4{};
-    }
   lds_loads_done();
-#pragma unroll
-  for (int t = 0; t < kGateTiles; ++t) {
-    if (t >= tiles) break;
-    f32x16 acc = f32x16{};
-    const u32x4* w = sw + t * kHalf + lane;
-#pragma unroll
-    for (int st = 0; st < 2 * CT; ++st) {
-      u32x4 a[P];
-#pragma unroll
-      for (int p = 0; p < P; ++p) a[p] = w[(st * P + p) * kBlk];
-      acc = mm_parts<BF>(a, xo[st], acc);
-    }
-    const int e = BF ? 0 : ex + eg[f0 + t];
+  for (int ft = f0; ft < f1; ++ft) {
+    const int odd = (ft - f0) & 1;
+    f32x4 bias[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int f = 32 * (f0 + t) + 8 * k + 4 * h;
-      f32x4 sv, dv;
+      const int f = 32 * ft + 8 * k + 4 * h;  // (F is a multiple of 16: a quad is inside or outside)
+      bias[k] = b && f < F ? *reinterpret_cast<const f32x4*>(b + f) : f32x4{};
+    }
+    if (ft + 1 < f1) fetch(ft + 1, odd ^ 1);
+    f32x16 acc = f32x16{};
+    stream_blocks<2 * CT, P, 3>(sw + odd * kHalf + lane,
+                                [&](int st, const u32x4* wa) { acc = mm_parts<BF>(wa, xo[st], acc); });
+    const int e = BF ? 0 : ex + eg[ft];
+    f32x4 sv[4], dv[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int f = 32 * ft + 8 * k + 4 * h;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float s1, d1;
-        gate_act((BF ? acc[4 * k + i] : ldexpf(acc[4 * k + i], e)) + bias[t][k][i], act, s1, d1);
-        sv[i] = f < F ? s1 : 0.f;
-        dv[i] = f < F ? d1 : 0.f;
-      }
-      if (n < N) {
-        *reinterpret_cast<f32x4*>(s + size_t(n) * ffn_stride(FT) + f) = sv;
-        if (ds) *reinterpret_cast<f32x4*>(ds + size_t(n) * ffn_stride(FT) + f) = dv;
+        gate_act((BF ? acc[4 * k + i] : ldexpf(acc[4 * k + i], e)) + bias[k][i], act, s1, d1);
+        sv[k][i] = f < F ? s1 : 0.f;
+        dv[k][i] = f < F ? d1 : 0.f;
       }
     }
+    // the next tile's weights are waited for before this tile's values are
+    // written: the writes then drain beside the next products
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    if (n < N)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const size_t at = size_t(n) * ffn_stride(FT) + 32 * ft + 8 * k + 4 * h;
+        *reinterpret_cast<f32x4*>(s + at) = sv[k];
+        if (ds) *reinterpret_cast<f32x4*>(ds + at) = dv[k];
+      }
+    __syncthreads();
   }
 }
 
@@ -607,29 +607,33 @@ __device__ __forceinline__ void bf16_parts(float (&v)[8], u32x4 (&op)[3]) {
     }
 }
 
-// grad W_gate = x[:, 0]^T dq: a wave takes 32 channels and two tiles of hidden
+// grad W_gate = x[:, 0]^T dq: a wave takes W tiles of channels and two of hidden
 // units over a range of nodes, sixteen nodes a step (lane half h the nodes 8 h
 // .. 8 h + 7) with the next step's loads in flight; 32x32x16 bf16 MFMA over
 // the bf16 parts of dq and of fp32 features, the products down to 2^-16 of the
-// first (six for fp32, three for bf16).  The waves of the first channel tile
-// also sum dq (grad b).  partial [S][C + 1][ffn_stride(FT)]: the last row is grad b.
-template <bool BF>
+// first (six for fp32, three for bf16).  Bound by the vector work that makes the
+// parts, which two tiles of channels share.  The waves of the first channel
+// tiles also sum dq (grad b).  partial [S][C + 1][ffn_stride(FT)]: the last row
+// is grad b.
+template <bool BF, int W>
 __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, int FT, const void* __restrict__ x,
                                                  const float* __restrict__ row_sum, const float* __restrict__ slope,
                                                  float* __restrict__ partial) {
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int FP = (FT + 1) / 2, t = blockIdx.x * 4 + wave;
-  if (t >= CT * FP) return;
-  const int ct = t / FP, ft = 2 * (t - ct * FP), c = 32 * ct + l32, Fp = ffn_stride(FT);
+  if (t >= (CT + W - 1) / W * FP) return;
+  const int ct = W * (t / FP), ft = 2 * (t % FP), c = 32 * ct + l32, Fp = ffn_stride(FT);
   const int n0 = int(int64_t(blockIdx.y) * N / gridDim.y), n1 = int(int64_t(blockIdx.y + 1) * N / gridDim.y);
-  const bool two = ft + 1 < FT, in_c = c < C;
-  f32x16 acc[2] = {f32x16{}, f32x16{}};
+  const bool two = ft + 1 < FT;
+  f32x16 acc[W][2];
+#pragma unroll
+  for (int w = 0; w < W; ++w) acc[w][0] = acc[w][1] = f32x16{};
   float sum[2] = {0.f, 0.f};
   struct Step {
     float b[2][8], c[2][8];  // the sum over rows and act'(q), whose product is dq
-    float a[8];
-    uint16_t ab[8];
+    float a[W][8];
+    uint16_t ab[W][8];
   };
   // nodes n .. n + 15; behind the range's end zeros (of the last node's address)
   auto load = [&](int n, Step& s) {
@@ -640,11 +644,15 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int o = min(8 * h + k, n1 - 1 - n);
-      const uint32_t at = uint32_t(o) * Fp + l32, xo = uint32_t(o) * d * C + (in_c ? c : 0);
-      if constexpr (BF)
-        s.ab[k] = (static_cast<const uint16_t*>(x) + xr)[xo];
-      else
-        s.a[k] = (static_cast<const float*>(x) + xr)[xo];
+      const uint32_t at = uint32_t(o) * Fp + l32, xo = uint32_t(o) * d * C;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const uint32_t xc = xo + (c + 32 * w < C ? c + 32 * w : 0);
+        if constexpr (BF)
+          s.ab[w][k] = (static_cast<const uint16_t*>(x) + xr)[xc];
+        else
+          s.a[w][k] = (static_cast<const float*>(x) + xr)[xc];
+      }
       s.b[0][k] = rs[at];
       s.c[0][k] = sl[at];
       s.b[1][k] = (rs + second)[at];
@@ -655,7 +663,7 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
   load(n0, cur);
   for (int n = n0; n < n1; n += 16) {
     if (n + 16 < n1) load(n + 16, nxt);
-    u32x4 av[3];
+    u32x4 av[W][3];
     float dq[2][8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -665,16 +673,23 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
         dq[j][k] = on ? cur.b[j][k] * cur.c[j][k] : 0.f;
         sum[j] += dq[j][k];
       }
-      if constexpr (BF)
-        cur.ab[k] = on && in_c ? cur.ab[k] : uint16_t(0);
-      else
-        cur.a[k] = on && in_c ? cur.a[k] : 0.f;
-    }
-    if constexpr (BF) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) av[0][k] = uint32_t(cur.ab[2 * k]) | uint32_t(cur.ab[2 * k + 1]) << 16;
-    } else {
-      bf16_parts(cur.a, av);
+      for (int w = 0; w < W; ++w) {
+        const bool in = on && c + 32 * w < C;
+        if constexpr (BF)
+          cur.ab[w][k] = in ? cur.ab[w][k] : uint16_t(0);
+        else
+          cur.a[w][k] = in ? cur.a[w][k] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if constexpr (BF) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) av[w][0][k] = uint32_t(cur.ab[w][2 * k]) | uint32_t(cur.ab[w][2 * k + 1]) << 16;
+      } else {
+        bf16_parts(cur.a[w], av[w]);
+      }
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -683,7 +698,9 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
 #pragma unroll
       for (int order = 2; order >= 0; --order)  // the small products first
 #pragma unroll
-        for (int p = 0; p <= (BF ? 0 : order); ++p) acc[j] = mm<true>(av[p], bv[order - p], acc[j]);
+        for (int p = 0; p <= (BF ? 0 : order); ++p)
+#pragma unroll
+          for (int w = 0; w < W; ++w) acc[w][j] = mm<true>(av[w][p], bv[order - p], acc[w][j]);
     }
     cur = nxt;
   }
@@ -692,10 +709,12 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
     if (j == 1 && !two) break;
     float* out = partial + size_t(blockIdx.y) * (C + 1) * Fp + 32 * (ft + j) + l32;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int cc = 32 * ct + acc_row(v, h);
-      if (cc < C) out[size_t(cc) * Fp] = acc[j][v];
-    }
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int cc = 32 * (ct + w) + acc_row(v, h);
+        if (cc < C) out[size_t(cc) * Fp] = acc[w][j][v];
+      }
     sum[j] = halves_sum(sum[j]);
     if (ct == 0 && h == 0) out[size_t(C) * Fp] = sum[j];
   }
@@ -1162,6 +1181,15 @@ RowsPlan rows_plan(int M, const Layout& l) {
   if (p.rem > 0) p.shares = std::max(1, std::min({slots / p.rem, l.FT / 4, 8}));
   return p;
 }
+// Tiles of channels a wave of k_ffn_dwg, and its workgroups over the weights:
+// two where the nodes' ranges of 64 or more still give two workgroups a CU
+// (8192 nodes, 256 -> 1024, fp32: 71 us with one, 56 with two; 957 nodes,
+// 80 -> 240: 8.1 and 10.5).
+int dwg_groups_of(const Layout& l, int W) { return ((l.CT + W - 1) / W * ((l.FT + 1) / 2) + 3) / 4; }
+int dwg_tiles(const Layout& l, int N) {
+  return l.CT > 1 && int64_t(dwg_groups_of(l, 2)) * ((N + 63) / 64) >= 2 * device_cus() ? 2 : 1;
+}
+int dwg_groups(const Layout& l, int N) { return dwg_groups_of(l, dwg_tiles(l, N)); }
 // packs: up, down, gate (forward); W_up and W_down^T as up, W_up^T as down,
 // gate, W_gate^T as down (backward)
 Layout layout(const FfnShape& p, bool backward) {
@@ -1187,7 +1215,7 @@ Layout layout(const FfnShape& p, bool backward) {
     o += gate;
     l.r0 = o;
     // shares of F, so that there is a workgroup a CU
-    l.KS = std::min({4, l.FT, std::max(1, device_cus() / ((p.N + 127) / 128 + 1))});
+    l.KS = std::min({4, l.FT, std::max(1, device_cus() / std::max(1, (p.N + 127) / 128))});
     o += al256(size_t(l.KS) * p.N * p.C * 4);
     // one workgroup a CU over the ranges of rows; a range has a node at least
     const int per = wgrad_tiles(l.CT, p.bf16), fb = (l.FT + per - 1) / per;
@@ -1196,8 +1224,7 @@ Layout layout(const FfnShape& p, bool backward) {
     if (l.S < 1) l.S = 1;
     l.part = o;
     o += al256(size_t(l.S) * 2 * p.C * ffn_stride(l.FT) * 4);
-    const int blocks = (l.CT * ((l.FT + 1) / 2) + 3) / 4;
-    int sg = 2 * device_cus() / blocks;
+    const int sg = std::max(1, 2 * device_cus() / dwg_groups(l, p.N));
     const int cap = (p.N + 63) / 64;  // at least 64 nodes a range
     l.Sg = sg < cap ? sg : cap;
     if (l.Sg < 1) l.Sg = 1;
@@ -1228,29 +1255,21 @@ hipError_t pack(const PackArgs& a, const Layout& l, const FfnShape& p, hipStream
   return hipGetLastError();
 }
 
-template <int CT, bool BF, int T>
-hipError_t gate_t(const Layout& l, const FfnShape& p, const void* x, char* ws, int slot, const float* b, bool slope,
-                  hipStream_t s) {
-  const dim3 grid((p.N + 127) / 128, (l.FT + T - 1) / T);
-  constexpr int lds = T * 2 * CT * (BF ? 1 : 2) * kBlk * 16;
-  auto k = k_ffn_gate<CT, BF, T>;
-  const hipError_t e =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return e;
-  k<<<grid, dim3(256), lds, s>>>(p.N, p.d, p.C, p.F, l.FT, p.act, x, reinterpret_cast<const u32x4*>(ws + l.pack[slot]),
-                                 reinterpret_cast<const int*>(ws + l.exps) + slot * l.FT, b,
-                                 reinterpret_cast<float*>(ws + l.s),
-                                 slope ? reinterpret_cast<float*>(ws + l.ds) : nullptr);
-  return hipGetLastError();
-}
-// Two tiles a workgroup read the features half as often (8192 x 256 -> 1024: 361
-// against 372 us for the backward); one where two would leave CUs idle (957 x
-// 16 x 80 -> 240: 80 against 74 us).
 template <int CT, bool BF>
 hipError_t gate(const Layout& l, const FfnShape& p, const void* x, char* ws, int slot, const float* b, bool slope,
                 hipStream_t s) {
-  const bool two = int64_t((p.N + 127) / 128) * ((l.FT + 1) / 2) >= 2 * device_cus();
-  return two ? gate_t<CT, BF, 2>(l, p, x, ws, slot, b, slope, s) : gate_t<CT, BF, 1>(l, p, x, ws, slot, b, slope, s);
+  // shares of F, so that there are two workgroups a CU
+  const int groups = (p.N + 127) / 128, shares = std::max(1, std::min(l.FT, 2 * device_cus() / groups));
+  constexpr int lds = 2 * 2 * CT * (BF ? 1 : 2) * kBlk * 16;
+  auto k = k_ffn_gate<CT, BF>;
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  k<<<dim3(groups, shares), dim3(256), lds, s>>>(
+      p.N, p.d, p.C, p.F, l.FT, p.act, x, reinterpret_cast<const u32x4*>(ws + l.pack[slot]),
+      reinterpret_cast<const int*>(ws + l.exps) + slot * l.FT, b, reinterpret_cast<float*>(ws + l.s),
+      slope ? reinterpret_cast<float*>(ws + l.ds) : nullptr);
+  return hipGetLastError();
 }
 
 template <bool BF>
@@ -1362,8 +1381,8 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   }
   float* part_g = reinterpret_cast<float*>(ws + l.part_g);
   if (a.grad_w_gate || a.grad_b_gate) {
-    k_ffn_dwg<BF><<<dim3((l.CT * ((l.FT + 1) / 2) + 3) / 4, l.Sg), dim3(256), 0, s>>>(p.N, p.d, p.C, l.CT, l.FT, a.x,
-                                                                                     sum, slope, part_g);
+    auto k = dwg_tiles(l, p.N) == 2 ? k_ffn_dwg<BF, 2> : k_ffn_dwg<BF, 1>;
+    k<<<dim3(dwg_groups(l, p.N), l.Sg), dim3(256), 0, s>>>(p.N, p.d, p.C, l.CT, l.FT, a.x, sum, slope, part_g);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
