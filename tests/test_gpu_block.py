@@ -1,0 +1,173 @@
+"""The operators of a pre-norm block run together on the GPU, as a network
+would use them:
+
+    x1 = x + attention(layer_norm(x)),  y = x1 + gated_ffn(layer_norm(x1)),
+
+forward and backward, against the oracle (float64).
+
+Tolerances.  Stage by stage the oracle takes the GPU's own inputs of that stage
+and the stage is held to its own bound (the parity bounds of its tests).  The
+whole block's gradient is then compared with central differences of the float64
+oracle along a direction v: four backward stages, each within 1e-5 of a node's
+largest gradient, and their sums of two (the residuals), which at most double
+what came before; 1e-4 of sum_n max|grad_n| sum|v_n| covers them."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_01131_amd as tdn
+import workloads
+from oracle import attention, block
+from tests._gpu_helpers import TOL_F32, check_elementwise, check_rows, random_factors
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+
+def _t(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+class Block:
+    """One block's parameters and graph, its steps on the GPU and the oracle."""
+
+    def __init__(self, seed, L, C, R, H, N, E, F):
+        w = workloads.random_graph(700 + seed, n_nodes=N, n_edges=E, L=L, C=C, R=R, sort=False)
+        rng = np.random.default_rng(seed)
+        f = lambda *s, k=1.0: (rng.standard_normal(s) * k).astype(np.float32)  # noqa: E731
+        self.L, self.r_cut, self.ei, self.vec = L, w["r_cut"], w["edge_index"], w["edge_vec"]
+        A, B, D = random_factors(L, R, seed)
+        n_radial = w["radial_w"].shape[0]
+        self.att = dict(A=A, B=B, D=D, W=w["W"], radial_w=w["radial_w"], W1=f(2 * C + n_radial, 16, k=0.1),
+                        w2=f(16, H, k=0.5))
+        self.g1, self.b1, self.g2, self.b2 = 1 + f(L + 1, C, k=0.2), f(C, k=0.2), 1 + f(L + 1, C, k=0.2), f(C, k=0.2)
+        self.ffn = dict(w_up=f(C, F, k=C ** -0.5), w_gate=f(C, F, k=C ** -0.5), w_down=f(F, C, k=F ** -0.5))
+        self.b_gate = f(F, k=0.3)
+        self.x, self.gy = f(N, (L + 1) ** 2, C), f(N, (L + 1) ** 2, C)
+        self.dev = {k: _t(v) for k, v in dict(g1=self.g1, b1=self.b1, g2=self.g2, b2=self.b2, b_gate=self.b_gate,
+                                              vec=self.vec, ei=self.ei, x=self.x, gy=self.gy, **self.att,
+                                              **self.ffn).items()}
+
+    def run(self, x, gy, ws=None):
+        """Every tensor of a forward and backward step; ws a workspace that
+        all calls share."""
+        p = self.dev
+        ffn = [p[k] for k in ("w_up", "w_gate", "w_down")]
+        s = {}
+        s["h1"] = tdn.layer_norm(x, p["g1"], p["b1"], eps=EPS)
+        res, _ = tdn.attention_forward(s["h1"], p["vec"], p["ei"], p["A"], p["B"], p["D"], p["W"], p["radial_w"],
+                                       p["W1"], p["w2"], L=self.L, r_cut=self.r_cut, z=torch.empty_like(x),
+                                       workspace=ws)
+        s["a"], s["x1"] = res.out, x + res.out
+        s["h2"] = tdn.layer_norm(s["x1"], p["g2"], p["b2"], eps=EPS)
+        s["y"] = tdn.gated_ffn(s["h2"], *ffn, b_gate=p["b_gate"], residual=s["x1"], workspace=ws)
+        s["gh2"], *s["g_ffn"] = tdn.gated_ffn_backward(s["h2"], *ffn, gy, b_gate=p["b_gate"], workspace=ws)
+        s["gx1"], *s["g_n2"] = tdn.layer_norm_backward(s["x1"], p["g2"], s["gh2"], eps=EPS, grad_res=gy, workspace=ws)
+        s["gh1"], *s["g_att"] = tdn.attention_backward(res, s["gx1"], workspace=ws)
+        s["gx"], *s["g_n1"] = tdn.layer_norm_backward(x, p["g1"], s["gh1"], eps=EPS, grad_res=s["gx1"], workspace=ws)
+        return s
+
+    def graph_args(self):
+        a = self.att
+        return (self.ei, self.vec, a["A"], a["B"], a["D"], a["W"], a["radial_w"], a["W1"], a["w2"], self.r_cut, self.L)
+
+    def ffn_args(self):
+        return [self.ffn[k].astype(np.float64) for k in ("w_up", "w_gate", "w_down")]
+
+    def oracle(self, x):
+        x1 = x + attention.forward(block.layer_norm(x, self.g1, self.b1, EPS), *self.graph_args())[0]
+        return block.gated_ffn(block.layer_norm(x1, self.g2, self.b2, EPS), *self.ffn_args(), self.b_gate, x1)
+
+
+SHAPES = [(1, 2, 32, 32, 1, 40, 400, 64), (2, 4, 64, 64, 2, 30, 500, 144), (3, 3, 128, 100, 4, 25, 300, 48)]
+
+
+def _tensors(s):
+    return [t for v in s.values() for t in (v if isinstance(v, list) else [v])]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"L{s[1]}C{s[2]}H{s[4]}")
+def test_forward_and_backward_stage_by_stage(shape):
+    b = Block(*shape)
+    s = b.run(b.dev["x"], b.dev["gy"])
+    n = {k: _np(v) for k, v in s.items() if not isinstance(v, list)}
+    # no hidden value of the attention near its activation's kink
+    src, dst = b.ei.astype(np.int64)
+    inv = n["h1"][:, 0]
+    C = inv.shape[1]
+    part = inv[dst] @ b.att["W1"][:C] + inv[src] @ b.att["W1"][C:2 * C]
+    from oracle.layer import radial_basis
+    phi, _ = radial_basis(np.linalg.norm(b.vec.astype(np.float64), axis=1), b.r_cut, b.att["radial_w"].shape[0])
+    assert np.abs(part + phi @ b.att["W1"][2 * C:]).min() > 1e-6
+    check_rows(n["h1"], block.layer_norm(b.x.astype(np.float64), b.g1, b.b1, EPS), TOL_F32, "h1")
+    check_rows(n["a"], attention.forward(n["h1"], *b.graph_args())[0], TOL_F32, "attention")
+    check_rows(n["h2"], block.layer_norm(n["x1"], b.g2, b.b2, EPS), TOL_F32, "h2")
+    check_rows(n["y"], block.gated_ffn(n["h2"], *b.ffn_args(), b.b_gate, n["x1"]), TOL_F32, "y")
+    gy = b.gy.astype(np.float64)
+    ref = block.gated_ffn_backward(n["h2"], *b.ffn_args(), gy, b.b_gate)
+    check_rows(n["gh2"], ref[0], TOL_F32, "grad h2")
+    for g, r in zip(s["g_ffn"], ref[1:]):
+        check_elementwise(_np(g), r, TOL_F32, "feed-forward weights")
+    ref = block.layer_norm_backward(n["x1"], b.g2, n["gh2"], EPS, gy)
+    check_rows(n["gx1"], ref[0], TOL_F32, "grad x1")
+    for g, r in zip(s["g_n2"], ref[1:]):
+        check_elementwise(_np(g), r, TOL_F32, "norm weights")
+    ref = attention.backward(n["h1"], *b.graph_args(), n["gx1"])
+    check_rows(n["gh1"], ref[0], TOL_F32, "grad h1")
+    check_elementwise(_np(s["g_att"][0]), ref[1], TOL_F32, "grad W")
+    ref = block.layer_norm_backward(b.x.astype(np.float64), b.g1, n["gh1"], EPS, n["gx1"])
+    check_rows(n["gx"], ref[0], TOL_F32, "grad x")
+    for g, r in zip(s["g_n1"], ref[1:]):
+        check_elementwise(_np(g), r, TOL_F32, "norm weights")
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"L{s[1]}C{s[2]}H{s[4]}")
+def test_the_gradient_against_differences(shape):
+    b = Block(*shape)
+    g = _np(b.run(b.dev["x"], b.dev["gy"])["gx"])
+    rng, x = np.random.default_rng(5), b.x.astype(np.float64)
+    for _ in range(3):
+        v = rng.choice([-1.0, 1.0], size=x.shape)
+        h = 1e-6
+        slope = ((b.oracle(x + h * v) - b.oracle(x - h * v)) * b.gy).sum() / (2 * h)
+        bound = 1e-4 * (np.abs(g).max(axis=(1, 2)) * np.abs(v).sum(axis=(1, 2))).sum()
+        assert abs((g * v).sum() - slope) <= bound
+
+
+def test_a_captured_step_with_one_shared_workspace():
+    b = Block(*SHAPES[1])
+    x, gy = b.dev["x"], b.dev["gy"]
+    ref = _tensors(b.run(x, gy))
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for _ in range(2):  # two graphs on one workspace, replayed in turn
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = b.run(x, gy, ws)
+        graphs.append((graph, _tensors(out)))
+    for k in range(3):
+        if k == 2:
+            x.copy_(x.flip(0))
+            ref = _tensors(b.run(x, gy))
+        for graph, out in graphs:
+            ws.fill_(255)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(out, ref))
+
+
+def test_two_blocks_on_two_streams():
+    one, two = Block(*SHAPES[0]), Block(*SHAPES[1])
+    refs = [_tensors(b.run(b.dev["x"], b.dev["gy"])) for b in (one, two)]
+    torch.cuda.synchronize()
+    outs = []
+    for b in (one, two):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            outs.append([_tensors(b.run(b.dev["x"], b.dev["gy"])) for _ in range(4)])
+    torch.cuda.synchronize()
+    for out, ref in zip(outs, refs):
+        assert all(torch.equal(p, q) for o in out for p, q in zip(o, ref))

@@ -174,3 +174,14 @@ def test_repeat_calls_streams_in_place_and_graph_replays(dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, ref))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,L,C,F,act,bias", [
+    (8500, 1, 32, 256, "silu", True),    # the last row tiles share out F; degree-0 sums joined before
+    (33300, 0, 48, 272, "gelu", False),  # ... and every row of degree 0
+    (2100, 0, 256, 1024, "silu", True),  # two channel tiles a wave of the gate's weights' gradient
+    (1400, 4, 64, 144, "sigmoid", True),
+])
+def test_more_rows_than_the_device_takes_at_once(N, L, C, F, act, bias, dtype):
+    _run_and_check(_inputs(N + L, N, L, C, F, dtype, bias), act, dtype)
