@@ -126,16 +126,19 @@ __global__ __launch_bounds__(256) void k_att_g(int E, int R, int nr, float sigma
 
 // ---- softmax and MLP: one wave a destination, one lane a hidden unit.  The
 // workgroup's sums of grad w2 and of the radial rows of grad W1 go to partial
-// [gridDim.x][n_radial + H][F].
+// [gridDim.x][n_radial + H][F].  NR and NH: n_radial and H in whole quads, so that
+// the loops over them hold no idle steps and several workgroups' records fit a
+// CU's LDS.
 constexpr int kDaWaves = 4;
+template <int NR, int NH>
 __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
     int N, int C, int F, int H, int nr, float sigma, const int32_t* __restrict__ offsets,
     const int32_t* __restrict__ perm, const int32_t* __restrict__ src, const float* __restrict__ edge_vec,
     const float* __restrict__ Pt, const float* __restrict__ Ps, const float* __restrict__ W1,
     const float* __restrict__ w2, const float* __restrict__ alpha, const float* __restrict__ dal,
     float* __restrict__ dhid, float* __restrict__ dPt, float* __restrict__ grad_vec, float* __restrict__ partial) {
-  __shared__ float s_da[kDaWaves][kWave][kMaxH];
-  __shared__ float s_phi[kDaWaves][kWave][kMaxRadial], s_psi[kDaWaves][kWave][kMaxRadial];
+  __shared__ float s_da[kDaWaves][kWave][NH];
+  __shared__ float s_phi[kDaWaves][kWave][NR], s_psi[kDaWaves][kWave][NR];
   __shared__ float s_dl[kDaWaves][kWave];
   __shared__ int s_eid[kDaWaves][kWave], s_src[kDaWaves][kWave];
   __shared__ float s_red[kDaWaves][kWave];
@@ -143,14 +146,14 @@ __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool unit = lane < F;
   const float* Wphi = W1 + size_t(2 * C) * F;
-  float wp[kMaxRadial], wo[kMaxH], gp[kMaxRadial], go[kMaxH];
+  float wp[NR], wo[NH], gp[NR], go[NH];
 #pragma unroll
-  for (int q = 0; q < kMaxRadial; ++q) {
+  for (int q = 0; q < NR; ++q) {
     wp[q] = unit && q < nr ? Wphi[q * F + lane] : 0.f;
     gp[q] = 0.f;
   }
 #pragma unroll
-  for (int k = 0; k < kMaxH; ++k) {
+  for (int k = 0; k < NH; ++k) {
     wo[k] = unit && k < H ? w2[lane * H + k] : 0.f;
     go[k] = 0.f;
   }
@@ -159,9 +162,9 @@ __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
     const int e0 = offsets[t], e1 = offsets[t + 1];
     float dpt = 0.f;
     if (e0 < e1) {
-      float dot[kMaxH];
+      float dot[NH];
 #pragma unroll
-      for (int k = 0; k < kMaxH; ++k) {
+      for (int k = 0; k < NH; ++k) {
         dot[k] = 0.f;
         if (k < H) {
           for (int e = e0 + lane; e < e1; e += kWave) dot[k] = fmaf(alpha[size_t(e) * H + k], dalpha(e, k), dot[k]);
@@ -181,7 +184,7 @@ __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
           s_eid[wv][lane] = eid;
           s_src[wv][lane] = src[eid];
 #pragma unroll
-          for (int k = 0; k < kMaxH; ++k)
+          for (int k = 0; k < NH; ++k)
             s_da[wv][lane][k] = k < H ? alpha[size_t(e) * H + k] * (dalpha(e, k) - dot[k]) : 0.f;
           vx = edge_vec[3 * size_t(eid)];
           vy = edge_vec[3 * size_t(eid) + 1];
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
           const float len = sqrtf(vx * vx + vy * vy + vz * vz);
           inv = 1.f / len;
 #pragma unroll
-          for (int q = 0; q < kMaxRadial; ++q) {
+          for (int q = 0; q < NR; ++q) {
             const float phi = q < nr ? radial_phi(len, q, sigma) : 0.f;
             s_phi[wv][lane][q] = phi;
             s_psi[wv][lane][q] = q < nr ? -radial_t(len, q, sigma) / sigma * phi : 0.f;
@@ -201,18 +204,18 @@ __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
           const float ps_next = unit && i + 1 < cnt ? Ps[size_t(s_src[wv][i + 1]) * F + lane] : 0.f;
           float hid = pt + ps, w = 0.f, dact = 0.f;
 #pragma unroll
-          for (int q = 0; q < kMaxRadial; ++q) {
+          for (int q = 0; q < NR; ++q) {
             hid = fmaf(s_phi[wv][i][q], wp[q], hid);
             w = fmaf(s_psi[wv][i][q], wp[q], w);
           }
 #pragma unroll
-          for (int k = 0; k < kMaxH; ++k) dact = fmaf(s_da[wv][i][k], wo[k], dact);
+          for (int k = 0; k < NH; ++k) dact = fmaf(s_da[wv][i][k], wo[k], dact);
           const float dh = hid > 0.f ? dact : kLeaky * dact, act = hid > 0.f ? hid : kLeaky * hid;
           dpt += dh;
 #pragma unroll
-          for (int q = 0; q < kMaxRadial; ++q) gp[q] = fmaf(s_phi[wv][i][q], dh, gp[q]);
+          for (int q = 0; q < NR; ++q) gp[q] = fmaf(s_phi[wv][i][q], dh, gp[q]);
 #pragma unroll
-          for (int k = 0; k < kMaxH; ++k) go[k] = fmaf(act, s_da[wv][i][k], go[k]);
+          for (int k = 0; k < NH; ++k) go[k] = fmaf(act, s_da[wv][i][k], go[k]);
           if (unit) dhid[size_t(s_eid[wv][i]) * F + lane] = dh;
           if (grad_vec) {
             const float dl = both_halves(half_sum(dh * w));
@@ -234,9 +237,9 @@ __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(
   }
   // the workgroup's sums over its waves, in order
 #pragma unroll
-  for (int i = 0; i < kMaxRadial + kMaxH; ++i) {
-    const bool radial = i < kMaxRadial;
-    const int k = radial ? i : i - kMaxRadial;
+  for (int i = 0; i < NR + NH; ++i) {
+    const bool radial = i < NR;
+    const int k = radial ? i : i - NR;
     if (k >= (radial ? nr : H)) continue;
     __syncthreads();
     s_red[wv][lane] = radial ? gp[radial ? k : 0] : go[radial ? 0 : k];
@@ -413,9 +416,11 @@ hipError_t launch_att_bwd_mlp(const AttBwdArgs& a, hipStream_t s) {
       a.C % kTile)
     return hipErrorInvalidValue;
   const int nb = att_bwd_da_blocks(a.N), rows = a.n_radial + a.H;
-  k_att_da<<<dim3(nb), dim3(kDaWaves * kWave), 0, s>>>(
-      a.N, a.C, a.F, a.H, a.n_radial, a.sigma, a.offsets, a.perm, a.src, a.edge_vec,
-      a.Pt, a.Ps, a.W1, a.w2, a.alpha, a.dal, a.dhid, a.dPt, a.grad_vec, a.part_da);
+  auto k = a.H <= 4 ? k_att_da<16, 4> : k_att_da<16, 8>;
+  if (a.n_radial <= 8) k = a.H <= 4 ? k_att_da<8, 4> : k_att_da<8, 8>;
+  k<<<dim3(nb), dim3(kDaWaves * kWave), 0, s>>>(a.N, a.C, a.F, a.H, a.n_radial, a.sigma, a.offsets, a.perm, a.src,
+                                                a.edge_vec, a.Pt, a.Ps, a.W1, a.w2, a.alpha, a.dal, a.dhid, a.dPt,
+                                                a.grad_vec, a.part_da);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   k_att_dps<<<dim3((a.N + 3) / 4), dim3(256), 0, s>>>(a.N, a.F, a.H, a.off_src, a.perm_src, a.dhid, a.alpha_eid, a.dPs,
