@@ -40,7 +40,8 @@ constexpr float kLeaky = 0.2f;
 
 // ---- the factors A and D [d, R] in the packed K order of
 // launch_feature_layout_packed: [pk_blocks][rank tile][64 lanes] x 16 bytes,
-// each rank's column in two fp16 parts of its values 2^-e, and 2^e [32 RT].
+// each rank's column in two fp16 parts of its values 2^-e, and 2^e [32 RT].  A
+// thread makes one block's word: only the latency of its loads counts (4 us).
 __global__ __launch_bounds__(256) void k_att_factors(int d, int R, int RT, const float* __restrict__ A,
                                                      const float* __restrict__ D, u32x4* __restrict__ ops,
                                                      float* __restrict__ scale) {
@@ -51,23 +52,22 @@ __global__ __launch_bounds__(256) void k_att_factors(int d, int R, int RT, const
   const float* F = which == 0 ? A : D;
   float mx = 0.f;
   if (r < R)
+#pragma unroll 9
     for (int k = 0; k < d; ++k) mx = fmaxf(mx, fabsf(F[size_t(k) * R + r]));
   const int e = f16_split_exponent(mx);
   const float sc = ldexpf(1.f, -e);
-  if (h == 0) scale[which * RT * kTile + r] = ldexpf(1.f, e);
+  if (h == 0 && blockIdx.y == 0) scale[which * RT * kTile + r] = ldexpf(1.f, e);
   auto value = [&](int slot) {  // the factor's value of a lane's K slot
     const int part = slot / n, row = h * n + slot - part * n;
     const float v = part < 3 && row < d && r < R ? F[size_t(row) * R + r] * sc : 0.f;
     const float hi = float(_Float16(v));
     return part == 2 ? v - hi : hi;
   };
-  u32x4* out = ops + size_t(which) * nb * RT * kWave;
-  for (int b = 0; b < nb; ++b) {
-    u32x4 w;
+  const int b = blockIdx.y;
+  u32x4 w;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = pack_f16x2_rne(value(8 * b + 2 * k), value(8 * b + 2 * k + 1));
-    out[(size_t(b) * RT + rt) * kWave + lane] = w;
-  }
+  for (int k = 0; k < 4; ++k) w[k] = pack_f16x2_rne(value(8 * b + 2 * k), value(8 * b + 2 * k + 1));
+  ops[(size_t(which * nb + b) * RT + rt) * kWave + lane] = w;
 }
 
 // ---- g_e [E, R] by sorted position: one thread a rank, harmonics and radial
@@ -302,6 +302,7 @@ __global__ __launch_bounds__(256) void k_att_dx0(int N, int d, int C, int F, con
   float acc[kDxNodes];
 #pragma unroll
   for (int k = 0; k < kDxNodes; ++k) acc[k] = 0.f;
+#pragma unroll 4
   for (int j = 0; j < F; ++j) {
     const float wt = W1[size_t(c) * F + j], ws = W1[size_t(C + c) * F + j];
 #pragma unroll
@@ -374,7 +375,8 @@ hipError_t launch_att_bwd_dg(const AttBwdArgs& a, hipStream_t s) {
   const int d = a.d, RT = (a.R + kTile - 1) / kTile;
   u32x4* ops = static_cast<u32x4*>(a.ops);
   float* f_scale = reinterpret_cast<float*>(ops + size_t(2) * pk_blocks(d) * RT * kWave);
-  k_att_factors<<<dim3((2 * RT * kWave + 255) / 256), dim3(256), 0, s>>>(d, a.R, RT, a.A, a.D, ops, f_scale);
+  k_att_factors<<<dim3((2 * RT * kWave + 255) / 256, pk_blocks(d)), dim3(256), 0, s>>>(d, a.R, RT, a.A, a.D, ops,
+                                                                                    f_scale);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   switch (a.L) {
