@@ -263,7 +263,7 @@ __global__ __launch_bounds__(256) void k_att_dps(int N, int F, int H, const int3
   const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (s >= N) return;
   const int e0 = offsets[s], e1 = offsets[s + 1];
-  for (int i = e0 * H + lane; i < e1 * H; i += kWave)
+  for (int64_t i = int64_t(e0) * H + lane; i < int64_t(e1) * H; i += kWave)
     alpha_src[i] = alpha_eid[size_t(perm[i / H]) * H + i % H];
   float v = 0.f;
   const bool unit = lane < F;

@@ -70,11 +70,12 @@ __device__ __forceinline__ float group_sum(float v, int G) {
 
 // One degree of one node.  `first` (uniform) is the element where the
 // workgroup's nodes start, `lane` the lane's offset from there (0 where the
-// lane is off: it takes part in its group's sums with zeros).
+// lane is off: it takes part in its group's sums with zeros).  y may be x: a
+// degree's rows are read before they are written.
 template <int l, bool BF>
 __device__ __forceinline__ void fwd_degree(bool on, size_t first, uint32_t lane, int C, int c, int G, float eps,
-                                           const void* __restrict__ x, const float* __restrict__ gamma,
-                                           const float* __restrict__ beta, void* __restrict__ y) {
+                                           const void* x, const float* __restrict__ gamma,
+                                           const float* __restrict__ beta, void* y) {
   constexpr int R = 2 * l + 1;
   const float inv_n = 1.f / float(R * C);
   const size_t at = first + size_t(l * l) * C;
@@ -103,9 +104,9 @@ __device__ __forceinline__ void fwd_degree(bool on, size_t first, uint32_t lane,
 }
 
 template <int L, bool BF>
-__global__ __launch_bounds__(kNormThreads) void k_norm_fwd(int N, int C, int G, float eps, const void* __restrict__ x,
+__global__ __launch_bounds__(kNormThreads) void k_norm_fwd(int N, int C, int G, float eps, const void* x,
                                                            const float* __restrict__ gamma,
-                                                           const float* __restrict__ beta, void* __restrict__ y) {
+                                                           const float* __restrict__ beta, void* y) {
   constexpr int d = (L + 1) * (L + 1);
   const int per = kNormThreads / G, c = 4 * int(threadIdx.x % G);
   const int64_t n0 = int64_t(blockIdx.x) * per;
