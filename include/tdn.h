@@ -478,8 +478,8 @@ tdn_status tdn_gated_ffn_forward(const tdn_ffn_problem* p, const void* x, const 
  * recomputed (the forward saves nothing; residual's gradient is grad_y).  Any
  * output may be NULL: grad_x [N, d, C], grad_w_up and grad_w_gate [C, F] and
  * grad_w_down [F, C] in the problem's dtype, grad_b_gate [F] f32.  With
- * TDN_BF16, u * act(q), (grad_y w_down^T) * act(q) and dq are each rounded to
- * bf16 once, the outputs once.  Sums over nodes run in a fixed order.  Outputs
+ * TDN_BF16, u * act(q), (grad_y w_down^T) * act(q) and, where it adds to
+ * grad_x, dq are each rounded to bf16 once, the outputs once.  Sums over nodes run in a fixed order.  Outputs
  * must not overlap inputs.  n_nodes = 0 zeroes the weights' gradients. */
 tdn_status tdn_gated_ffn_backward(const tdn_ffn_problem* p, const void* x, const void* w_up, const void* w_gate,
                                   const float* b_gate, const void* w_down, const void* grad_y, void* grad_x,

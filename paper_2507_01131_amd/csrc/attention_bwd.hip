@@ -41,7 +41,8 @@ constexpr float kLeaky = 0.2f;
 // ---- the factors A and D [d, R] in the packed K order of
 // launch_feature_layout_packed: [pk_blocks][rank tile][64 lanes] x 16 bytes,
 // each rank's column in two fp16 parts of its values 2^-e, and 2^e [32 RT].  A
-// thread makes one block's word: only the latency of its loads counts (4 us).
+// thread makes one block's word: only the latency of its loads counts (6 us; 17
+// where a thread made all blocks).
 __global__ __launch_bounds__(256) void k_att_factors(int d, int R, int RT, const float* __restrict__ A,
                                                      const float* __restrict__ D, u32x4* __restrict__ ops,
                                                      float* __restrict__ scale) {
@@ -71,7 +72,8 @@ __global__ __launch_bounds__(256) void k_att_factors(int d, int R, int RT, const
 }
 
 // ---- g_e [E, R] by sorted position: one thread a rank, harmonics and radial
-// basis of 64 edges at a time in LDS, read sixteen bytes at a time.
+// basis of 64 edges at a time in LDS, read sixteen bytes at a time.  151 k
+// edges, R = 128, L = 4: 36 us, 77 MB written; bound by the vector work of B^T Y.
 constexpr int kGEdges = 64;
 template <int L>
 __global__ __launch_bounds__(256) void k_att_g(int E, int R, int nr, float sigma, const int32_t* __restrict__ perm,
@@ -127,8 +129,9 @@ __global__ __launch_bounds__(256) void k_att_g(int E, int R, int nr, float sigma
 // ---- softmax and MLP: one wave a destination, one lane a hidden unit.  The
 // workgroup's sums of grad w2 and of the radial rows of grad W1 go to partial
 // [gridDim.x][n_radial + H][F].  NR and NH: n_radial and H in whole quads, so that
-// the loops over them hold no idle steps and several workgroups' records fit a
-// CU's LDS.
+// the loops over them hold no idle steps and more workgroups' records fit a CU's
+// LDS (8 and 4 for 3200 molecules' edges: 46 us; 78 with room for 16 and 8).
+// Bound by the latency of an edge's chain at the few waves that N gives.
 constexpr int kDaWaves = 4;
 template <int NR, int NH>
 __global__ __launch_bounds__(kDaWaves* kWave) void k_att_da(

@@ -55,7 +55,9 @@ __device__ __forceinline__ float lane_value(float v, int lane) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
-// waves a SIMD that the registers allow
+// waves a SIMD that the registers allow: three at C = 64 (960 molecules' edges, the
+// whole backward: 266 us, 270 with two), two above (C = 128: 1190 us, 1480 with
+// three, which spill)
 __host__ __device__ constexpr int dg_waves(int CT) { return CT <= 2 ? 3 : 2; }
 
 // sixteen-byte words of a slot: a node's, in whole direct loads of a wave
@@ -65,8 +67,13 @@ __host__ __device__ constexpr int dg_slot(int ct_n, int n) { return (ct_n * 16 *
 // The range is a stream of items, x[s_e] of every edge and, before the first
 // edge of each destination, Gz[t]: one node's packed words each, brought into
 // one of two LDS slots by direct loads while the item before is worked on, so
-// that each item is read from L2 once for all ranks.  Bound by the matrix
-// instructions and, beside them, the sums of U V.
+// that each item is read from L2 once for all ranks.  Channel tiles and tiles a
+// head are known when it is compiled: the sums of U V of a tile run beside the
+// matrix products of the next (3200 molecules' 151 k edges, L = 4, C = R = 128,
+// four heads: 485 us; the whole backward 1228, 1272 with loops over runtime
+// counts).  Bound by the vector
+// work and the matrix instructions together, which two waves a SIMD overlap in
+// part: about 210 and 150 us of that time.
 template <int L, int CT, int PH>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(dg_waves(CT)))) void k_att_dg(DgArgs a) {
   constexpr int d = (L + 1) * (L + 1), n = pk_rows(d), nb = pk_blocks(d), n4 = n / 4, nt = n % 4;

@@ -224,7 +224,8 @@ __device__ __forceinline__ void to_operand(const float (&t)[16], int bias, int& 
 //   up:   [ft][2 CT K-steps][parts] blocks, lane (h, l32), value i:
 //         w(16 st + 8 h + i, 32 ft + l32)
 //   down: [ft][CT][2 K-steps][parts] blocks: w(32 ct + l32, 32 ft + acc_krow(q, h, i))
-// fp32 problems: in two fp16 parts of w 2^-e, e[ft] stored.
+// fp32 problems: in two fp16 parts of w 2^-e, e[ft] stored.  The five of the
+// backward at 256 -> 1024 take 9 us, most of it latency: one workgroup a tile.
 struct PackArgs {
   const void* W[5];
   u32x4* out[5];
@@ -312,7 +313,8 @@ __device__ __forceinline__ void lds_loads_done() {
 // s = act(q) and, if asked for, act'(q), [N, ffn_stride(FT)] fp32 each: a workgroup
 // takes 128 nodes (lanes) and a share of the tiles of hidden units, the next
 // tile's weights on their way to LDS while this one's are used.  Bound by the
-// writes of s and act'(q) and the reads of the weights.
+// writes of s and act'(q) and the reads of the weights (8192 nodes, 256 -> 1024,
+// fp32 with act'(q): 36 us, 67 MB written; 4096 nodes, bf16: 15 us).
 template <int CT, bool BF>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_ffn_gate(
     int N, int d, int C, int F, int FT, int act, const void* __restrict__ x, const u32x4* __restrict__ wg,
@@ -402,7 +404,8 @@ __host__ __device__ constexpr int rows_waves(int CT, bool BF) { return CT <= (BF
 // tile's u beside the conversion of h needed its registers (bf16, 102400 x 256 ->
 // 1024: 227 us with it, 178 without).  Bound by the LDS reads of the weights,
 // which every wave makes for its own 32 rows: as many cycles as the matrix
-// instructions.  Row tiles that would leave CUs idle have the tiles of F shared
+// instructions (that bf16 size: 140 us, 0.77 PFLOP/s; fp32, 80000 x 128 -> 512:
+// 75 us, 0.84 PFLOP/s of part products).  Row tiles that would leave CUs idle have the tiles of F shared
 // out, and k_ffn_join adds the shares' sums.
 template <int CT, bool BF>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(CT, BF)))) void k_ffn_rows(RowsArgs a) {
@@ -500,7 +503,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(rows_waves(
     }
 }
 
-// The shares' sums in order, with the residuals, four channels a thread.
+// The shares' sums in order, with the residuals, four channels a thread.  Bound
+// by memory (8192 x 256 in four shares with four of residual0: 12 us).
 template <bool BF>
 __global__ __launch_bounds__(256) void k_ffn_join(RowsArgs a) {
   const size_t before = size_t(a.full) * 128 * a.C, total = size_t(a.M) * a.C - before;
@@ -523,7 +527,8 @@ __global__ __launch_bounds__(256) void k_ffn_join(RowsArgs a) {
 // ------------------------------------------------------ the gate's gradients
 // r0 = dq W_gate^T, the sums over gridDim.y shares of F apart: [gridDim.y, N, C].
 // A workgroup takes 128 nodes; the packed weights go through LDS as in
-// k_ffn_rows.
+// k_ffn_rows.  Bound by the reads of sum and act'(q) at one workgroup a CU (8192
+// nodes, 1024 -> 256, fp32: 35 us, 67 MB).
 template <int CT, bool BF>
 __global__ __launch_bounds__(256) void k_ffn_dx0(int N, int C, int FT, const float* __restrict__ sum,
                                                  const float* __restrict__ slope, const u32x4* __restrict__ wg,
@@ -612,7 +617,7 @@ __device__ __forceinline__ void bf16_parts(float (&v)[8], u32x4 (&op)[3]) {
 // .. 8 h + 7) with the next step's loads in flight; 32x32x16 bf16 MFMA over
 // the bf16 parts of dq and of fp32 features, the products down to 2^-16 of the
 // first (six for fp32, three for bf16).  Bound by the vector work that makes the
-// parts, which two tiles of channels share.  The waves of the first channel
+// parts, which two tiles of channels share (8192 nodes, 256 -> 1024, fp32: 54 us).  The waves of the first channel
 // tiles also sum dq (grad b).  partial [S][C + 1][ffn_stride(FT)]: the last row
 // is grad b.
 template <bool BF, int W>
@@ -731,11 +736,18 @@ struct WgradArgs {
   float* partial;                 // [gridDim.y][2][C][ffn_stride(FT)]: W_down's (as [c][f]), then W_up's
 };
 
+// A tile of 32 rows of x and grad_y is brought to registers a tile ahead, split
+// into parts, written to LDS in both operand orders, and read from there by
+// every wave.  The phases (write, first products, exchange for dq, second
+// products) stand between barriers, which bounds the kernel: 4096 x 25 rows,
+// 256 -> 1024, bf16: 420 us, 0.51 PFLOP/s; 8192 x 1, fp32: 157 us, 0.33 PFLOP/s of
+// part products.
 // Eight waves, two a SIMD: a wave's packed weights and sums fit 256 registers
 // with a pair of waves to a tile of 32 hidden units up to 128 fp32 channels
 // (256 bf16 ones).  Above, four waves share a tile: each role's two take half
 // of the contraction over channels, exchange the halves of u and dh through
-// LDS, and take half of the channels of the sums.
+// LDS, and take half of the channels of the sums (8192 nodes, 256 -> 1024: 528 us
+// for the backward with pairs, whose registers spilled, 477 with halves).
 constexpr int kWgradWaves = 8;
 __host__ __device__ constexpr bool wgrad_halves(int CT, bool BF) { return !BF && CT > 4; }
 __host__ __device__ constexpr int wgrad_tiles(int CT, bool BF) { return wgrad_halves(CT, BF) ? 2 : 4; }
@@ -1169,9 +1181,11 @@ struct Layout {
   int CT, FT, P, S, Sg, KS;
   size_t pack_bytes;
 };
-// The row tiles of k_ffn_rows: as many rounds of the device's workgroups as they
-// fill, then the tiles that are left, with F shared out over the device, four
-// tiles of F a share at least.
+// The row tiles of k_ffn_rows: as many rounds of one workgroup a CU as they fill,
+// then the tiles that are left, with F shared out over the device, four tiles of
+// F a share at least (measured on an earlier loop over F: 800 row tiles, bf16, F =
+// 1024: 229 us without shares, 204 with; 625 tiles, fp32, F = 512: 97 and 92, and
+// 104 with shares for two workgroups a CU).
 struct RowsPlan {
   int full, rem, shares;
 };
@@ -1369,8 +1383,10 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   w.partial = reinterpret_cast<float*>(ws + l.part);
   {
     const size_t lds = size_t(wgrad_words(CT, BF, p.d)) * 16;
-    // tiles of whole nodes where a node's rows fill most of one: no sums of
-    // rows through LDS and one value of the gate a lane
+    // tiles of whole nodes where a node's rows fill half of one or more: no sums
+    // of rows through LDS and one value of the gate a lane (4096 x 25 x 256 -> 1024
+    // in bf16: 754 us for the backward without, 634 with); below, whole nodes
+    // would leave most rows of a tile empty
     auto k = p.d >= 16 ? k_ffn_wgrad<CT, BF, true> : k_ffn_wgrad<CT, BF, false>;
     e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     if (e != hipSuccess) return e;

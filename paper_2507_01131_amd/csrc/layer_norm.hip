@@ -21,6 +21,11 @@
 // its nodes, are added in LDS over the workgroup's groups and then over the
 // workgroups, each in a fixed order.  Statistics, sums and products are fp32;
 // a bf16 output is rounded once, when it is stored.
+//
+// Measured: forward 3200 x 25 x 128 fp32, 82 MB: 15 us (5.5 TB/s, at a copy's
+// rate); backward 4960 x 49 x 128 fp32 with grad_res, 498 MB: 113 us and 6 us for
+// the sums (4.4 TB/s; a copy's 5.1 would take 97); 4096 x 25 x 256 bf16, 210 MB:
+// 53 + 5 us.
 #include "common.hpp"
 #include "kernels.h"
 
