@@ -726,9 +726,38 @@ __global__ __launch_bounds__(256) void k_ffn_dwg(int N, int d, int C, int CT, in
 }
 
 // ------------------------------------------------------- weights' gradients
+// fp32 rows of x and grad_y in two fp16 parts, as k_ffn_wgrad's operands take
+// them: each four channels as 16 bytes, the high parts' two words, then the low
+// parts', of values 2^-e; e a row's exponent (kNoRow for a row of zeros).  Done
+// once here, not by every workgroup that takes the rows (131072 x 256 -> 1024: 1970
+// us for the backward with the parts made there, 1780 so; 957 x 16 x 80 -> 240: 75
+// and 77).  G lanes (C / 4 rounded up to a power of two) take a row.  Bound by
+// memory (8192 x 256: 8 us).
+constexpr int kNoRow = -100000;
+__global__ __launch_bounds__(256) void k_ffn_split(int M, int C, int G, const float* __restrict__ x,
+                                                   const float* __restrict__ gy, u32x4* __restrict__ out_x,
+                                                   u32x4* __restrict__ out_gy, int* __restrict__ exps) {
+  const int64_t row = int64_t(blockIdx.x) * (256 / G) + threadIdx.x / G;
+  const int c = 4 * int(threadIdx.x % G);
+  const bool on = row < M && c < C;
+  const size_t at = size_t(on ? row : 0) * C + (on ? c : 0);
+  const f32x4 v = on ? *reinterpret_cast<const f32x4*>((blockIdx.y ? gy : x) + at) : f32x4{};
+  float mx = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+  for (int o = G >> 1; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  if (!on) return;
+  const int e = f16_split_exponent(mx);
+  const float sc = ldexpf(1.f, -e);
+  uint32_t hi0, hi1, lo0, lo1;
+  split_f16x2_pair(v[0] * sc, v[1] * sc, hi0, lo0);
+  split_f16x2_pair(v[2] * sc, v[3] * sc, hi1, lo1);
+  (blockIdx.y ? out_gy : out_x)[at / 4] = u32x4{hi0, hi1, lo0, lo1};
+  if (c == 0) exps[size_t(blockIdx.y) * M + row] = mx > 0.f ? e : kNoRow;
+}
+
 struct WgradArgs {
   int N, d, C, FT;
-  const void *x, *gy;             // [N d, C]
+  const void *x, *gy;             // [N d, C]: bf16, or the parts of k_ffn_split
+  const int* e_rows;              // [2][N d]: the parts' exponents, of x, then of grad_y
   const u32x4 *up_u, *up_d;       // W_up and W_down^T packed as `up`
   const int *e_u, *e_d;
   const float* s;                 // act(q) [N, ffn_stride(FT)]
@@ -736,12 +765,12 @@ struct WgradArgs {
   float* partial;                 // [gridDim.y][2][C][ffn_stride(FT)]: W_down's (as [c][f]), then W_up's
 };
 
-// A tile of 32 rows of x and grad_y is brought to registers a tile ahead, split
-// into parts, written to LDS in both operand orders, and read from there by
-// every wave.  The phases (write, first products, exchange for dq, second
+// A tile of 32 rows of x and grad_y is brought to registers a tile ahead, written
+// to LDS in both operand orders, and read from there by every wave.  The phases (write, first products, exchange for dq, second
 // products) stand between barriers, which bounds the kernel: 4096 x 25 rows,
-// 256 -> 1024, bf16: 420 us, 0.51 PFLOP/s; 8192 x 1, fp32: 157 us, 0.33 PFLOP/s of
-// part products.
+// 256 -> 1024, bf16: 420 us, 0.51 PFLOP/s; 8192 x 1, fp32: 134 us, 0.38 PFLOP/s of
+// part products.  (Two buffers of operands and one barrier less: 532 us for the
+// bf16 backward instead of 561, but 381 instead of 366 at C = 128: not taken.)
 // Eight waves, two a SIMD: a wave's packed weights and sums fit 256 registers
 // with a pair of waves to a tile of 32 hidden units up to 128 fp32 channels
 // (256 bf16 ones).  Above, four waves share a tile: each role's two take half
@@ -768,10 +797,10 @@ __host__ __device__ constexpr int wgrad_words(int CT, bool BF, int d) {
          (wgrad_halves(CT, BF) ? 0 : wgrad_tiles(CT, BF) * 4 * kBlk + 2 * 32 * ((wgrad_nodes(d) + 1) / 2 * 2));
 }
 
-// four channels of a row as they lie in memory
+// four channels of a row as they lie in memory: both parts' words, or bf16
 template <bool BF>
 struct Raw4 {
-  f32x4 v;
+  u32x4 v;
 };
 template <>
 struct Raw4<true> {
@@ -789,7 +818,6 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
   constexpr int kPack = 2 * CT * P * kBlk;  // of a packed tile
   constexpr int kItems = (64 * CT + NT - 1) / NT;  // 4 x 4 blocks of a 32-row tile per thread and tensor
   extern __shared__ u32x4 smem[];
-  __shared__ uint32_t s_max[2][32];
   __shared__ float s_rowf[32];
   __shared__ int s_eb;
   u32x4* sU = kHalves ? smem : smem + 4 * kOp;  // [wave of role 0, or every wave][4][64]
@@ -866,7 +894,7 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
     if constexpr (BF)
       return Raw4<BF>{*reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + row * C + i)};
     else
-      return Raw4<BF>{*reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + row * C + i)};
+      return Raw4<BF>{*reinterpret_cast<const u32x4*>(static_cast<const uint32_t*>(p) + row * C + i)};
   };
   // the gate's values of the nodes of rows mb .. mb + 31 counted from node nb
   auto fetch_gate = [&](int nb, int mb, int buf) {
@@ -885,6 +913,7 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
     asm volatile("" : "+v"(t));
     return t;
   };
+  int e_row = kNoRow;  // (first wave) of a tile's row l32: of x and, in the other half, of grad_y
   auto fetch = [&](int rb, int n) {  // rows rb .. rb + n - 1 of a tile
     const int t0 = here();
 #pragma unroll
@@ -898,18 +927,22 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
         vg[k][r] = on ? raw(a.gy, size_t(rb + r), at) : Raw4<BF>{};
       }
     }
+    if constexpr (!BF)
+      if (wave == 0) e_row = l32 < n ? a.e_rows[size_t(h) * a.N * d + rb + l32] : kNoRow;
   };
   // a 4 x 4 block into both operand orders
-  auto put = [&](const Raw4<BF> (&v)[4], int rg, int c, u32x4* op, const float* sc) {
+  auto put = [&](const Raw4<BF> (&v)[4], int rg, int c, u32x4* op) {
     uint32_t hl[P][4][2];  // [part][row][pair of channels]
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        if constexpr (BF)
+        if constexpr (BF) {
           hl[0][r][k] = k == 0 ? v[r].v.x : v[r].v.y;
-        else
-          split_f16x2_pair(v[r].v[2 * k] * sc[r], v[r].v[2 * k + 1] * sc[r], hl[0][r][k], hl[1][r][k]);
+        } else {
+          hl[0][r][k] = v[r].v[k];
+          hl[1][r][k] = v[r].v[2 + k];
+        }
       }
     const int st = c >> 4, hh = (c >> 3) & 1;
     const int ct = c >> 5, q = rg >> 2, ht = rg & 1, it = (rg >> 1) & 1;
@@ -929,7 +962,6 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
       }
     }
   };
-  if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
   int prev = 0;         // rows of the tile before, whose products wait in sP
   int nb = n0, mb = 0;  // the tile's first row: row mb of node nb
   int buf = 0;
@@ -951,35 +983,12 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
   int rows = tile_rows(r0, 0);
   fetch(r0, rows);
   for (int rb = r0; rb < r1;) {
-    __syncthreads();  // s_max is zero; the tile before is consumed
+    __syncthreads();  // the tile before is consumed
     if constexpr (!BF) {
-#pragma unroll
-      for (int k = 0; k < kItems; ++k) {
-        const int i = tid + NT * k, rg = i / (8 * CT);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float mx = 0.f, mg = 0.f;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            mx = fmaxf(mx, fabsf(vx[k][r].v[c]));
-            mg = fmaxf(mg, fabsf(vg[k][r].v[c]));
-          }
-#pragma unroll
-          for (int o = 4; o > 0; o >>= 1) {
-            mx = fmaxf(mx, __shfl_xor(mx, o));
-            mg = fmaxf(mg, __shfl_xor(mg, o));
-          }
-          if ((lane & 7) == 0 && i < 64 * CT) {
-            atomicMax(&s_max[0][4 * rg + r], __float_as_uint(mx));
-            atomicMax(&s_max[1][4 * rg + r], __float_as_uint(mg));
-          }
-        }
-      }
-      __syncthreads();
-      if (tid < 64) {
+      if (wave == 0) {
         // 2^(e_x + e_gy) of each row, relative to the largest of the tile's
-        const float mx = __uint_as_float(s_max[0][l32]), mg = __uint_as_float(s_max[1][l32]);
-        const int e = mx > 0.f && mg > 0.f ? f16_split_exponent(mx) + f16_split_exponent(mg) : kUnset;
+        const int other = __shfl_xor(e_row, 32);
+        const int e = e_row != kNoRow && other != kNoRow ? e_row + other : kUnset;
         int top = e;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o));
@@ -992,16 +1001,8 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
     for (int k = 0; k < kItems; ++k) {
       const int i = t0 + NT * k, rg = i / (8 * CT), c = 4 * (i - rg * 8 * CT);
       if (i < 64 * CT) {
-        float sx[4], sg[4];
-        if constexpr (!BF) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            sx[r] = ldexpf(1.f, -f16_split_exponent(__uint_as_float(s_max[0][4 * rg + r])));
-            sg[r] = ldexpf(1.f, -f16_split_exponent(__uint_as_float(s_max[1][4 * rg + r])));
-          }
-        }
-        put(vx[k], rg, c, smem, sx);
-        put(vg[k], rg, c, smem + kOp, sg);
+        put(vx[k], rg, c, smem);
+        put(vg[k], rg, c, smem + kOp);
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the gate's values too
@@ -1033,8 +1034,6 @@ __global__ __launch_bounds__(kWgradWaves* kWave) __attribute__((amdgpu_waves_per
       }
     }
     if (more) fetch(rb, rows);
-    if constexpr (!BF)
-      if (tid < 64) s_max[tid >> 5][tid & 31] = 0u;
     // u or dh of the tile: rows in registers, hidden units in lanes
     f32x16 t = f32x16{};
     stream_blocks<kSteps, P, 3, kBlkW>(rows_op, [&](int st, const u32x4* op) { t = mm_parts<BF>(op, w[st], t); });
@@ -1177,7 +1176,7 @@ __global__ __launch_bounds__(256) void k_ffn_wsum(int C, int F, int FT, int S, i
 size_t al256(size_t b) { return (b + 255) & ~size_t(255); }
 
 struct Layout {
-  size_t pack[5], exps, s, ds, sum, r0, part, part_g, rows, total;
+  size_t pack[5], exps, s, ds, sum, r0, part, part_g, rows, split_x, split_gy, e_rows, total;
   int CT, FT, P, S, Sg, KS;
   size_t pack_bytes;
 };
@@ -1244,6 +1243,13 @@ Layout layout(const FfnShape& p, bool backward) {
     if (l.Sg < 1) l.Sg = 1;
     l.part_g = o;
     o += al256(size_t(l.Sg) * (p.C + 1) * ffn_stride(l.FT) * 4);
+  }
+  if (backward && !p.bf16) {
+    const size_t bytes = al256(size_t(p.N) * p.d * p.C * 4);
+    l.split_x = o;
+    l.split_gy = o + bytes;
+    l.e_rows = o + 2 * bytes;
+    o += 2 * bytes + al256(size_t(2) * p.N * p.d * 4);
   }
   const RowsPlan r = rows_plan(p.N * p.d, l);
   l.rows = o;
@@ -1374,6 +1380,20 @@ hipError_t backward(const FfnShape& p, const FfnArgs& a, hipStream_t s) {
   w.FT = l.FT;
   w.x = a.x;
   w.gy = a.grad_y;
+  if constexpr (!BF) {
+    u32x4 *sx = reinterpret_cast<u32x4*>(ws + l.split_x), *sg = reinterpret_cast<u32x4*>(ws + l.split_gy);
+    int* e_rows = reinterpret_cast<int*>(ws + l.e_rows);
+    int G = 4;
+    while (4 * G < p.C) G <<= 1;
+    const int64_t M = int64_t(p.N) * p.d;
+    k_ffn_split<<<dim3(uint32_t((M * G + 255) / 256), 2), dim3(256), 0, s>>>(
+        int(M), p.C, G, static_cast<const float*>(a.x), static_cast<const float*>(a.grad_y), sx, sg, e_rows);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    w.x = sx;
+    w.gy = sg;
+    w.e_rows = e_rows;
+  }
   w.up_u = reinterpret_cast<const u32x4*>(ws + l.pack[0]);
   w.up_d = reinterpret_cast<const u32x4*>(ws + l.pack[1]);
   w.e_u = ex;
