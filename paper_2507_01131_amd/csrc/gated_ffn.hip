@@ -766,11 +766,12 @@ struct WgradArgs {
 };
 
 // A tile of 32 rows of x and grad_y is brought to registers a tile ahead, written
-// to LDS in both operand orders, and read from there by every wave.  The phases (write, first products, exchange for dq, second
-// products) stand between barriers, which bounds the kernel: 4096 x 25 rows,
-// 256 -> 1024, bf16: 420 us, 0.51 PFLOP/s; 8192 x 1, fp32: 134 us, 0.38 PFLOP/s of
-// part products.  (Two buffers of operands and one barrier less: 532 us for the
-// bf16 backward instead of 561, but 381 instead of 366 at C = 128: not taken.)
+// to LDS in both operand orders, and read from there by every wave.  The phases
+// (write, first products, exchange for dq, second products) stand between
+// barriers, which bounds the kernel: 4096 x 25 rows, 256 -> 1024, bf16: 420 us,
+// 0.51 PFLOP/s; 8192 x 1, fp32: 134 us, 0.38 PFLOP/s of part products.  (Two
+// buffers of operands and one barrier less: 532 us for the bf16 backward instead
+// of 561, but 381 instead of 366 at C = 128: not taken.)
 // Eight waves, two a SIMD: a wave's packed weights and sums fit 256 registers
 // with a pair of waves to a tile of 32 hidden units up to 128 fp32 channels
 // (256 bf16 ones).  Above, four waves share a tile: each role's two take half
