@@ -34,7 +34,6 @@ namespace tdn {
 namespace {
 
 constexpr int kNormThreads = 256;
-constexpr int kMaxNormL = 6;
 
 template <bool BF>
 __device__ __forceinline__ f32x4 load4(const void* p, size_t i) {

@@ -194,3 +194,31 @@ def test_refuses_another_result():
                         _t(w["radial_w"]), L=2, r_cut=w["r_cut"])
     with pytest.raises(ValueError):
         tdn.attention_backward(plain, _t(w["grad_out"]))
+
+
+def test_more_than_2_31_edge_ranks():
+    """Places beyond 32 bits in the [E, R] arrays: the last destinations' edges
+    of 8.5 million against the same edges alone."""
+    N, per, L, C, R, H, F = 20000, 425, 1, 32, 256, 1, 16
+    w = _problem(27, L, C, R, H, F, N, 40, True)
+    E, last = N * per, 8 * per
+    gen = torch.Generator("cuda").manual_seed(6)
+    dst = torch.arange(N, dtype=torch.int32, device="cuda").repeat_interleave(per)
+    src = torch.randint(0, N, (E,), generator=gen, device="cuda", dtype=torch.int32)
+    v = torch.randn((E, 3), generator=gen, device="cuda")
+    v *= (0.3 + 0.6 * torch.rand((E, 1), generator=gen, device="cuda")) * w["r_cut"] / v.norm(dim=1, keepdim=True)
+    A, B, D = w["factors"]
+    x, g = _t(w["x"]), _t(w["grad_out"])
+
+    def run(e0):
+        res, _ = tdn.attention_forward(x, v[e0:].clone(), torch.stack([src[e0:], dst[e0:]]), _t(A), _t(B), _t(D),
+                                       _t(w["W"]), _t(w["radial_w"]), _t(w["W1"]), _t(w["w2"]), L=L,
+                                       r_cut=w["r_cut"], edges_sorted=True, z=torch.empty_like(x))
+        return tdn.attention_backward(res, g)
+
+    big, alone = run(0), run(E - last)
+    assert all(torch.isfinite(t).all() for t in big)
+    a, b = big[2][-last:].cpu().numpy(), alone[2].cpu().numpy()
+    assert rel_err(a, b) < TOL_F32
+    del big, alone
+    torch.cuda.empty_cache()

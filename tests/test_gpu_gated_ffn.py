@@ -185,3 +185,32 @@ def test_repeat_calls_streams_in_place_and_graph_replays(dtype):
 ])
 def test_more_rows_than_the_device_takes_at_once(N, L, C, F, act, bias, dtype):
     _run_and_check(_inputs(N + L, N, L, C, F, dtype, bias), act, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,L,C,F", [(5, 2, 256, 4096), (1, 0, 16, 4096), (140, 0, 80, 4096)])
+def test_the_widest_hidden_layer(N, L, C, F, dtype):
+    _run_and_check(_inputs(N, N, L, C, F, dtype), "silu", dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_than_2_31_features(dtype):
+    """Places beyond 32 bits: the last nodes of 8.4 million against the oracle
+    (a node's output and gradient need no other node)."""
+    N, C, F = (1 << 23) + 1000, 256, 16
+    i = _inputs(3, 300, 0, C, F, dtype)
+    gen = torch.Generator("cuda").manual_seed(4)
+    x, gy = (torch.randn((N, 1, C), generator=gen, device="cuda", dtype=DT[dtype]) for _ in range(2))
+    x[-300:], gy[-300:] = i["x"], i["grad_y"]
+    w = [i[k] for k in ("w_up", "w_gate", "w_down")]
+    ref = [_np(t) for t in (i["x"], *w)]
+    bounds = _bf16_bounds(i, "silu") if dtype == "bf16" else [None] * 2
+    y = tdn.gated_ffn(x, *w, b_gate=i["b_gate"])
+    _check(y[-300:], block.gated_ffn(*ref, _np(i["b_gate"])), dtype, bounds[0], "y", True)
+    del y
+    grads = tdn.gated_ffn_backward(x, *w, gy, b_gate=i["b_gate"])
+    _check(grads[0][-300:], block.gated_ffn_backward(*ref, _np(i["grad_y"]), _np(i["b_gate"]))[0], dtype, bounds[1],
+           "grad_x", True)
+    assert all(torch.isfinite(g).all() for g in grads[1:])
+    del x, gy, grads
+    torch.cuda.empty_cache()

@@ -126,3 +126,21 @@ def test_repeat_calls_streams_in_place_and_graph_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(yg, y) and all(torch.equal(p, q) for p, q in zip(gg, grads))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_than_2_31_features(dtype):
+    """Places beyond 32 bits: the last nodes of 2.2 million against the oracle."""
+    N, L, C = (1 << 21) + 100000, 1, 256
+    x, g, b, dy, res = _inputs(4, 200, L, C, dtype)
+    gen = torch.Generator("cuda").manual_seed(5)
+    big, gy = (torch.randn((N, 4, C), generator=gen, device="cuda", dtype=DT[dtype]) for _ in range(2))
+    big[-200:], gy[-200:] = x, dy
+    y = tdn.layer_norm(big, g, b, eps=EPS)
+    _check(y[-200:], block.layer_norm(_np(x), _np(g), _np(b), EPS), dtype, "y")
+    del y
+    gx, gg, gb = tdn.layer_norm_backward(big, g, gy, eps=EPS)
+    _check(gx[-200:], block.layer_norm_backward(_np(x), _np(g), _np(dy), EPS)[0], dtype, "grad_x")
+    assert torch.isfinite(gg).all() and torch.isfinite(gb).all()
+    del big, gy, gx
+    torch.cuda.empty_cache()
